@@ -12,7 +12,11 @@
  *   3. the minibatch forward of Algorithm 2 with the max-margin loss (Eq. 1),
  *   4. hard negative items for training queries (Sec. 3.3),
  *   5. the MapReduce-inference variant of Sec. 3.4 (boards pool their pins,
- *      pins their boards, boards without features).
+ *      pins their boards, boards without features),
+ *   6. the training of dense layers over embeddings (the output layers of
+ *      Algorithm 2's final loop, or layers that follow them): forward and
+ *      backward passes, one weight or one per group of rows, and the
+ *      optimiser step that orthogonalises a layer's update.
  *
  * Conventions shared by every entry point
  *   - Graph (Sec. 3.1): a bipartite graph of pins I and boards C, V = I u C.
@@ -472,6 +476,125 @@ int pinsage_minibatch_forward(const pinsage_graph_t* graph, const pinsage_walk_p
                               void* z_out, int64_t* set_sizes, unsigned long long* total_steps,
                               void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- dense layers and their training -------------------------------------
+ * Activations of a dense layer; GELU is the tanh form
+ * 0.5 u (1 + tanh(sqrt(2/pi) (u + 0.044715 u^3))), SILU u / (1 + exp(-u)). */
+typedef enum {
+  PINSAGE_ACT_NONE = 0,
+  PINSAGE_ACT_RELU = 1,
+  PINSAGE_ACT_GELU = 2,
+  PINSAGE_ACT_SILU = 3
+} pinsage_activation_t;
+
+/* A dense layer over rows x_r (embeddings; Algorithm 2's final loop has two):
+ *   u_r = W x_r + b,   y_r = act(u_r) + residual_r
+ * num_groups = 0: one W [d_out][d_in] and b [d_out] for all rows, offsets NULL.
+ * num_groups = G >= 1: the rows come in G contiguous groups (node types,
+ * categories, experts), group g holding rows offsets[g] .. offsets[g+1] - 1,
+ * with its own W [d_out][d_in] and b [d_out] of W [G][d_out][d_in],
+ * b [G][d_out].
+ *   W        device, storage dtype, rows ldw elements apart (>= d_in)
+ *   b        device fp32, or NULL (no bias)
+ *   offsets  device int64 [G + 1], offsets[0] = 0, non-decreasing, at most n;
+ *            any group may be empty. Rows from offsets[G] on belong to no group:
+ *            their outputs (y, u, dx) are zeros and they add to no gradient.
+ *            Read on the device; values that break these rules give unspecified
+ *            results but no access outside the operands.
+ * Any sizes and row strides (leading dimensions, in elements) are accepted,
+ * rows need no alignment beyond their elements'; rows whose pointers and strides
+ * are multiples of 16 bytes are faster. Limits: 1 <= d_in, d_out <= 16384,
+ * leading dimensions <= 2^20, num_groups <= 4096, n < 2^31. */
+typedef struct {
+  int32_t d_in;
+  int32_t d_out;
+  int32_t num_groups;
+  pinsage_dtype_t dtype;
+  pinsage_activation_t activation;
+  const void* W;
+  int64_t ldw;
+  const float* b;
+  const int64_t* offsets;
+} pinsage_dense_t;
+
+/* The layer's forward pass over n rows. x: device [n][d_in], rows ldx apart;
+ * residual: device [n][d_out], rows ldr apart, or NULL (none); u: device
+ * [n][d_out], rows ldu apart, or NULL (not kept; a backward pass through an
+ * activation needs it); y: device [n][d_out], rows ldy apart; all in the
+ * storage dtype. y may be the residual itself (same pointer and stride);
+ * otherwise outputs overlap no input. Sums, bias, activation and residual in
+ * fp32, each output rounded once. A row's bits follow from its own values, its
+ * weight and the kernel that the sizes choose (few rows take another one). */
+int pinsage_dense_forward(const pinsage_dense_t* layer, const void* x, int64_t n, int64_t ldx,
+                          const void* residual, int64_t ldr, void* u, int64_t ldu, void* y,
+                          int64_t ldy, void* stream);
+
+/* Workspace bytes needed by pinsage_dense_backward for n rows. */
+int pinsage_dense_backward_workspace_size(const pinsage_dense_t* layer, int64_t n, size_t* bytes);
+
+/* The layer's gradients, for dy = the loss's gradient by y (which is also the
+ * residual's gradient):
+ *   dz_r = dy_r * act'(u_r),  dx_r = W^T dz_r,  dW = sum_r dz_r x_r^T,
+ *   db = sum_r dz_r   (per group; zeros for an empty one)
+ * dy: device [n][d_out], rows lddy apart; x as in the forward pass; u: the
+ * pre-activation it kept (NULL for PINSAGE_ACT_NONE; for RELU without a
+ * residual y serves as well); dx: device [n][d_in], rows lddx apart, or NULL;
+ * dW: device [d_out][d_in] ([G] of them), dense, or NULL; db: device fp32
+ * [d_out] ([G] of them) or NULL; a NULL output is not computed. dx, dW in the
+ * storage dtype, rounded once from fp32 sums; dz is rounded to the storage
+ * dtype for dx and dW (not for db). RELU's derivative at 0 is 0. Outputs
+ * overlap no input. Sums are added in a fixed order. workspace: device, >=
+ * pinsage_dense_backward_workspace_size bytes, 256-aligned. */
+int pinsage_dense_backward(const pinsage_dense_t* layer, const void* dy, int64_t lddy,
+                           const void* x, int64_t ldx, const void* u, int64_t ldu, int64_t n,
+                           void* dx, int64_t lddx, void* dW, float* db, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* Newton-Schulz orthogonalisation of `batch` matrices G [rows][cols]: with
+ * X [m][n] = G, or G^T where rows > cols,
+ *   X = G / (||G||_F + eps), then `steps` times
+ *   A = X X^T,  X = a X + (b A + c A A) X,
+ * returned in G's orientation: for (a, b, c) = (3.4445, -4.7750, 2.0315) and 5
+ * steps, singular values above about 0.01 of the norm end between 0.7 and 1.2.
+ * A zero matrix stays zero (eps > 0). Products on fp16 parts around a fixed
+ * scale: one part (2^-11) for bf16 storage, two (2^-22) for fp32; coefficients
+ * must keep X, A and b A + c A A below 16 in magnitude, as those above do, and
+ * a matrix whose norm is far below eps loses low bits (absolute 2^-36 of X).
+ * Limits: 1 <= rows, cols <= 16384, 1 <= steps <= 64, batch <= 65535. */
+typedef struct {
+  int64_t batch;
+  int32_t rows;
+  int32_t cols;
+  pinsage_dtype_t dtype;
+  int32_t steps;
+  float a, b, c;
+  float eps;
+} pinsage_newton_schulz_t;
+
+/* Workspace bytes needed by pinsage_orthogonalize and pinsage_muon_step. */
+int pinsage_newton_schulz_workspace_size(const pinsage_newton_schulz_t* params, size_t* bytes);
+
+/* in, out: device [batch][rows][cols], storage dtype (out may be in).
+ * workspace: device, >= the size above, 256-aligned. */
+int pinsage_orthogonalize(const pinsage_newton_schulz_t* params, const void* in, void* out,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* One optimiser step of `batch` weights of the same shape:
+ *   momentum' = beta momentum + grad
+ *   O  = the orthogonalisation of (nesterov ? grad + beta momentum' : momentum')
+ *   W' = (1 - lr weight_decay) W - lr scale O
+ * W, grad: device [batch][rows][cols], storage dtype; momentum: device fp32,
+ * the same shape. W_out and momentum_out may be W and momentum (in place). */
+typedef struct {
+  float lr;
+  float beta;
+  float weight_decay;
+  float scale;
+  int32_t nesterov;
+} pinsage_muon_t;
+int pinsage_muon_step(const pinsage_newton_schulz_t* params, const pinsage_muon_t* muon,
+                      const void* W, const void* grad, const float* momentum, void* W_out,
+                      float* momentum_out, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Per-kernel timing (hipEvents recorded around every launch on the launch
  * stream). pinsage_profile_enable(1) clears and starts collection;
  * pinsage_profile_read() synchronises the recorded events and returns, for
@@ -493,7 +616,10 @@ enum {
   PINSAGE_KERNEL_WALK_TABLE = 11, /* the walk table of pinsage_embed_all's walks */
   PINSAGE_KERNEL_POOL_W = 12, /* pool and W fused (DENSE_THEN_POOL, bf16,
                                  d_in = d_out = 256, top_t <= 64) */
-  PINSAGE_KERNEL_COUNT = 13
+  PINSAGE_KERNEL_DENSE = 13,      /* dense layers: forward */
+  PINSAGE_KERNEL_DENSE_GRAD = 14, /* dense layers: dz, db, dx, dW */
+  PINSAGE_KERNEL_NEWTON_SCHULZ = 15, /* a whole orthogonalisation or optimiser step */
+  PINSAGE_KERNEL_COUNT = 16
 };
 int pinsage_profile_enable(int on);
 int pinsage_profile_read(int kernel, int64_t* launches, double* total_ms);

@@ -20,10 +20,15 @@ from .api import (  # noqa: F401
     build_neighborhoods,
     convolve_layer,
     convolve_workspace_size,
+    dense_backward,
+    dense_backward_workspace_size,
+    dense_forward,
     embed_all,
     embed_all_workspace_size,
     hard_negatives,
     max_margin_loss,
+    muon_step,
+    orthogonalize,
     output_mlp,
     profile_enable,
     profile_read,

@@ -19,12 +19,13 @@ PINSAGE_F32, PINSAGE_BF16 = 0, 1
 PINSAGE_POOL_THEN_DENSE, PINSAGE_DENSE_THEN_POOL = 0, 1
 DATAFLOWS = {"pool_then_dense": PINSAGE_POOL_THEN_DENSE, "dense_then_pool": PINSAGE_DENSE_THEN_POOL}
 POOLS = {"importance": 0, "mean": 1, "max": 2}
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 (KERNEL_WALK, KERNEL_GEMM_Q, KERNEL_POOL, KERNEL_GEMM_W, KERNEL_MINIBATCH, KERNEL_LOSS,
  KERNEL_GEMM_R, KERNEL_MLP) = range(8)
 KERNEL_NAMES = ["walk_topt", "gemm_q", "pool", "gemm_w", "minibatch", "loss", "gemm_r", "mlp",
                 "hard_neg", "graph_nbr", "gemm_qr", "walk_table",
-                "pool_w"]
+                "pool_w", "dense", "dense_grad", "newton_schulz"]
 
 EXPORTED = [
     "pinsage_version", "pinsage_status_string", "pinsage_last_error",
@@ -39,6 +40,8 @@ EXPORTED = [
     "pinsage_minibatch_workspace_size", "pinsage_minibatch_forward",
     "pinsage_profile_enable", "pinsage_profile_read", "pinsage_profile_random_reads",
     "pinsage_profile_random_gathers", "pinsage_walk_table_size", "pinsage_build_walk_table",
+    "pinsage_dense_forward", "pinsage_dense_backward_workspace_size", "pinsage_dense_backward",
+    "pinsage_newton_schulz_workspace_size", "pinsage_orthogonalize", "pinsage_muon_step",
 ]
 
 
@@ -84,6 +87,25 @@ class Pairs(ctypes.Structure):
                 ("queries", ctypes.c_void_p), ("positives", ctypes.c_void_p),
                 ("negatives", ctypes.c_void_p), ("margin", ctypes.c_float),
                 ("num_hard", ctypes.c_int64), ("hard_negatives", ctypes.c_void_p)]
+
+
+class Dense(ctypes.Structure):
+    _fields_ = [("d_in", ctypes.c_int32), ("d_out", ctypes.c_int32),
+                ("num_groups", ctypes.c_int32), ("dtype", ctypes.c_int),
+                ("activation", ctypes.c_int), ("W", ctypes.c_void_p), ("ldw", ctypes.c_int64),
+                ("b", ctypes.c_void_p), ("offsets", ctypes.c_void_p)]
+
+
+class NewtonSchulz(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32),
+                ("dtype", ctypes.c_int), ("steps", ctypes.c_int32), ("a", ctypes.c_float),
+                ("b", ctypes.c_float), ("c", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class Muon(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_float), ("beta", ctypes.c_float),
+                ("weight_decay", ctypes.c_float), ("scale", ctypes.c_float),
+                ("nesterov", ctypes.c_int32)]
 
 
 class PinsageError(RuntimeError):
@@ -162,6 +184,16 @@ def lib():
                                                  ctypes.c_uint64, ctypes.c_void_p, ctypes.c_void_p]
     L.pinsage_walk_table_size.argtypes = [ctypes.POINTER(Graph), ctypes.POINTER(ctypes.c_size_t)]
     L.pinsage_build_walk_table.argtypes = [ctypes.POINTER(Graph), P, ctypes.c_size_t, P]
+    size_p = ctypes.POINTER(ctypes.c_size_t)
+    L.pinsage_dense_forward.argtypes = [ctypes.POINTER(Dense), P, i64, i64, P, i64, P, i64, P, i64,
+                                        P]
+    L.pinsage_dense_backward_workspace_size.argtypes = [ctypes.POINTER(Dense), i64, size_p]
+    L.pinsage_dense_backward.argtypes = [ctypes.POINTER(Dense), P, i64, P, i64, P, i64, i64, P,
+                                         i64, P, P, P, ctypes.c_size_t, P]
+    L.pinsage_newton_schulz_workspace_size.argtypes = [ctypes.POINTER(NewtonSchulz), size_p]
+    L.pinsage_orthogonalize.argtypes = [ctypes.POINTER(NewtonSchulz), P, P, P, ctypes.c_size_t, P]
+    L.pinsage_muon_step.argtypes = [ctypes.POINTER(NewtonSchulz), ctypes.POINTER(Muon), P, P, P, P,
+                                    P, P, ctypes.c_size_t, P]
     for name in EXPORTED:
         fn = getattr(L, name)
         if fn.restype is None or fn.restype is ctypes.c_int:

@@ -505,6 +505,204 @@ class Minibatch:
         return ctypes.byref(self._mlp) if self._mlp is not None else None
 
 
+# ---- dense layers and their training ---------------------------------------------------
+NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)  # (a, b, c) of the quintic iteration
+
+
+def _rows(t: torch.Tensor, name: str, n: int, width: int, dtype: torch.dtype) -> int:
+    """Checks a matrix [n, width] whose rows are contiguous; returns its row stride."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA (HIP) tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if t.dim() != 2 or t.shape[0] != n or t.shape[1] != width:
+        raise ValueError(f"{name} must be [{n}, {width}], got {list(t.shape)}")
+    ld, step = t.stride()
+    if width > 1 and step != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    if n <= 1:
+        return width
+    if ld < width:
+        raise ValueError(f"{name}'s rows must not overlap")
+    return ld
+
+
+def _dense(x_dtype: torch.dtype, W: torch.Tensor, b: Optional[torch.Tensor], activation: str,
+           offsets: Optional[torch.Tensor]) -> L.Dense:
+    act = L.ACTIVATIONS.get(activation)
+    if act is None:
+        raise ValueError(f"activation must be one of {sorted(L.ACTIVATIONS)}, got {activation!r}")
+    groups = 0
+    if offsets is not None:
+        _dev(offsets, "offsets", torch.int64)
+        groups = offsets.numel() - 1
+        if offsets.dim() != 1 or groups < 1:
+            raise ValueError("offsets must be [groups + 1] with at least one group")
+    if not isinstance(W, torch.Tensor) or not W.is_cuda:
+        raise ValueError("W must be a CUDA (HIP) tensor")
+    if W.dtype != x_dtype:
+        raise ValueError(f"W must have dtype {x_dtype}, got {W.dtype}")
+    if W.dim() != (3 if groups else 2) or (groups and W.shape[0] != groups):
+        raise ValueError("W must be [d_out, d_in], or [groups, d_out, d_in] with offsets")
+    d_out, d_in = W.shape[-2:]
+    ldw = W.stride(-2) if d_out > 1 else d_in
+    if (d_in > 1 and W.stride(-1) != 1) or ldw < d_in or (
+            groups > 1 and W.stride(0) != (d_out * ldw if d_out > 1 else d_in)):
+        raise ValueError("W must have contiguous rows, and its groups one after another")
+    if b is not None:
+        _dev(b, "b", torch.float32)
+        if b.numel() != max(1, groups) * d_out:
+            raise ValueError("b must have one entry per output (and group)")
+    return L.Dense(d_in, d_out, groups, _dtype_code(x_dtype), act, W.data_ptr(), ldw,
+                   b.data_ptr() if b is not None else None,
+                   offsets.data_ptr() if offsets is not None else None)
+
+
+def dense_forward(x: torch.Tensor, W: torch.Tensor, b: Optional[torch.Tensor] = None,
+                  activation: str = "none", residual: Optional[torch.Tensor] = None,
+                  offsets: Optional[torch.Tensor] = None, want_preact: bool = False,
+                  out: Optional[torch.Tensor] = None, stream=None):
+    """y = act(x W^T + b) + residual over the rows of x [n, d_in]; W [d_out, d_in], b [d_out]
+    fp32. With offsets (int64 [groups + 1], on the GPU) rows offsets[g] .. offsets[g + 1] - 1 take
+    W[g] of W [groups, d_out, d_in] and b[g]; rows past the last group become zero. x, W and the
+    residual share one dtype, float32 or bfloat16; matrices may have any row stride. activation:
+    "none", "relu", "gelu" (tanh form) or "silu". Returns y, or (y, u) with want_preact, u the
+    value before the activation, which dense_backward needs."""
+    d = _dense(x.dtype, W, b, activation, offsets)
+    n = int(x.shape[0])
+    ldx = _rows(x, "x", n, d.d_in, x.dtype)
+    ldr = _rows(residual, "residual", n, d.d_out, x.dtype) if residual is not None else 0
+    if out is None:
+        out = torch.empty((n, d.d_out), dtype=x.dtype, device=x.device)
+        ldy = d.d_out
+    else:
+        ldy = _rows(out, "out", n, d.d_out, x.dtype)
+    u = torch.empty((n, d.d_out), dtype=x.dtype, device=x.device) if want_preact else None
+    st = L.lib().pinsage_dense_forward(ctypes.byref(d), x.data_ptr(), n, ldx,
+                                       residual.data_ptr() if residual is not None else None, ldr,
+                                       u.data_ptr() if want_preact else None, d.d_out,
+                                       out.data_ptr(), ldy, _stream(stream))
+    if st:
+        L.check(st, "pinsage_dense_forward")
+    return (out, u) if want_preact else out
+
+
+def dense_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor,
+                   u: Optional[torch.Tensor] = None, activation: str = "none",
+                   offsets: Optional[torch.Tensor] = None, need_dx: bool = True,
+                   need_dW: bool = True, need_db: bool = True,
+                   workspace: Optional[torch.Tensor] = None, stream=None):
+    """Gradients (dx, dW, db) of dense_forward for dy, the loss's gradient by y (it is the
+    residual's gradient as well); u is the pre-activation that the forward pass kept (not needed
+    without an activation). Entries that are not needed are None. db is fp32, dx and dW have x's
+    dtype."""
+    d = _dense(x.dtype, W, None, activation, offsets)
+    n = int(x.shape[0])
+    ldx = _rows(x, "x", n, d.d_in, x.dtype)
+    lddy = _rows(dy, "dy", n, d.d_out, x.dtype)
+    ldu = 0
+    if activation != "none":
+        if u is None:
+            raise ValueError("u is needed for the gradient through an activation")
+        ldu = _rows(u, "u", n, d.d_out, x.dtype)
+    dx = torch.empty((n, d.d_in), dtype=x.dtype, device=x.device) if need_dx else None
+    dW = torch.empty(W.shape, dtype=x.dtype, device=x.device) if need_dW else None
+    db = torch.empty(W.shape[:-1], dtype=torch.float32, device=x.device) if need_db else None
+    if workspace is None:
+        need = ctypes.c_size_t(0)
+        L.check(L.lib().pinsage_dense_backward_workspace_size(ctypes.byref(d), n,
+                                                              ctypes.byref(need)),
+                "pinsage_dense_backward_workspace_size")
+        workspace = torch.empty(max(1, need.value), dtype=torch.uint8, device=x.device)
+    st = L.lib().pinsage_dense_backward(ctypes.byref(d), dy.data_ptr(), lddy, x.data_ptr(), ldx,
+                                        u.data_ptr() if u is not None else None, ldu, n,
+                                        _ptr(dx), d.d_in, _ptr(dW), _ptr(db),
+                                        workspace.data_ptr(), workspace.numel(), _stream(stream))
+    if st:
+        L.check(st, "pinsage_dense_backward")
+    return dx, dW, db
+
+
+def dense_backward_workspace_size(W: torch.Tensor, n: int, activation: str = "none",
+                                  offsets: Optional[torch.Tensor] = None) -> int:
+    """Workspace bytes of dense_backward over n rows."""
+    need = ctypes.c_size_t(0)
+    d = _dense(W.dtype, W, None, activation, offsets)
+    L.check(L.lib().pinsage_dense_backward_workspace_size(ctypes.byref(d), n, ctypes.byref(need)),
+            "pinsage_dense_backward_workspace_size")
+    return int(need.value)
+
+
+def _newton_schulz(t: torch.Tensor, name: str, steps: int, coefficients, eps: float):
+    _dev(t, name)
+    if t.dim() not in (2, 3):
+        raise ValueError(f"{name} must be [rows, cols] or [batch, rows, cols]")
+    batch = t.shape[0] if t.dim() == 3 else 1
+    a, b, c = coefficients
+    return L.NewtonSchulz(batch, t.shape[-2], t.shape[-1], _dtype_code(t.dtype), int(steps), a, b,
+                          c, eps)
+
+
+def _newton_schulz_workspace(p: L.NewtonSchulz, device) -> torch.Tensor:
+    need = ctypes.c_size_t(0)
+    L.check(L.lib().pinsage_newton_schulz_workspace_size(ctypes.byref(p), ctypes.byref(need)),
+            "pinsage_newton_schulz_workspace_size")
+    return torch.empty(max(1, need.value), dtype=torch.uint8, device=device)
+
+
+def orthogonalize(g: torch.Tensor, steps: int = 5, coefficients=NEWTON_SCHULZ, eps: float = 1e-7,
+                  out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                  stream=None) -> torch.Tensor:
+    """Newton-Schulz orthogonalisation of g [rows, cols] or of each g[i] of [batch, rows, cols]:
+    X = g / (|g|_F + eps), then `steps` times X = a X + (b A + c A A) X with A = X X^T (in the
+    orientation with fewer rows than columns)."""
+    p = _newton_schulz(g, "g", steps, coefficients, eps)
+    if out is None:
+        out = torch.empty_like(g)
+    elif _dev(out, "out", g.dtype).shape != g.shape:
+        raise ValueError("out must have g's shape")
+    if workspace is None:
+        workspace = _newton_schulz_workspace(p, g.device)
+    st = L.lib().pinsage_orthogonalize(ctypes.byref(p), g.data_ptr(), out.data_ptr(),
+                                       workspace.data_ptr(), workspace.numel(), _stream(stream))
+    if st:
+        L.check(st, "pinsage_orthogonalize")
+    return out
+
+
+def muon_step(W: torch.Tensor, grad: torch.Tensor, momentum: torch.Tensor, lr: float,
+              beta: float = 0.95, weight_decay: float = 0.0, scale: Optional[float] = None,
+              nesterov: bool = True, steps: int = 5, coefficients=NEWTON_SCHULZ,
+              eps: float = 1e-7, W_out: Optional[torch.Tensor] = None,
+              momentum_out: Optional[torch.Tensor] = None,
+              workspace: Optional[torch.Tensor] = None, stream=None):
+    """One optimiser step of a weight W [rows, cols] (or of a batch of them):
+    momentum' = beta momentum + grad; W' = (1 - lr weight_decay) W - lr scale O, O the
+    orthogonalised grad + beta momentum' (nesterov) or momentum'. scale: sqrt(max(1, rows / cols))
+    unless given. momentum is fp32. Writes W and momentum in place, or W_out and momentum_out;
+    returns both."""
+    p = _newton_schulz(W, "W", steps, coefficients, eps)
+    W_out = W if W_out is None else W_out
+    momentum_out = momentum if momentum_out is None else momentum_out
+    for t, name, dt in ((grad, "grad", W.dtype), (W_out, "W_out", W.dtype),
+                        (momentum, "momentum", torch.float32),
+                        (momentum_out, "momentum_out", torch.float32)):
+        if _dev(t, name, dt).shape != W.shape:
+            raise ValueError(f"{name} must have W's shape")
+    if scale is None:
+        scale = max(1.0, p.rows / p.cols) ** 0.5
+    m = L.Muon(lr, beta, weight_decay, scale, 1 if nesterov else 0)
+    if workspace is None:
+        workspace = _newton_schulz_workspace(p, W.device)
+    st = L.lib().pinsage_muon_step(ctypes.byref(p), ctypes.byref(m), W.data_ptr(),
+                                   grad.data_ptr(), momentum.data_ptr(), W_out.data_ptr(),
+                                   momentum_out.data_ptr(), workspace.data_ptr(),
+                                   workspace.numel(), _stream(stream))
+    if st:
+        L.check(st, "pinsage_muon_step")
+    return W_out, momentum_out
+
+
 def profile_enable(on: bool = True) -> None:
     L.check(L.lib().pinsage_profile_enable(1 if on else 0), "pinsage_profile_enable")
 

@@ -1699,3 +1699,289 @@ int pinsage_minibatch_forward(const pinsage_graph_t* graph, const pinsage_walk_p
 }
 
 }  // extern "C"
+
+// ---- dense layers and their training ---------------------------------------
+namespace pinsage {
+namespace {
+
+constexpr int64_t kMaxLd = 1ll << 20;
+
+int check_ld(const char* what, int64_t ld, int64_t width) {
+  if (ld < width)
+    return fail(PINSAGE_EINVAL, "%s: leading dimension %lld below the row's %lld", what,
+                (long long)ld, (long long)width);
+  if (ld > kMaxLd)
+    return fail(PINSAGE_EUNSUPPORTED, "%s: leading dimension %lld above 2^20", what, (long long)ld);
+  return PINSAGE_OK;
+}
+
+int check_dense(const pinsage_dense_t* d, int64_t n) {
+  if (!d) return fail(PINSAGE_EINVAL, "layer is NULL");
+  if (d->dtype != PINSAGE_F32 && d->dtype != PINSAGE_BF16)
+    return fail(PINSAGE_EINVAL, "unknown dtype %d", (int)d->dtype);
+  if (d->activation < PINSAGE_ACT_NONE || d->activation > PINSAGE_ACT_SILU)
+    return fail(PINSAGE_EINVAL, "unknown activation %d", (int)d->activation);
+  if (d->d_in < 1 || d->d_out < 1)
+    return fail(PINSAGE_EINVAL, "dims must be positive (%d, %d)", d->d_in, d->d_out);
+  if (d->d_in > 16384 || d->d_out > 16384)
+    return fail(PINSAGE_EUNSUPPORTED, "dims above 16384 (%d, %d)", d->d_in, d->d_out);
+  if (d->num_groups < 0) return fail(PINSAGE_EINVAL, "negative num_groups");
+  if (d->num_groups > 4096) return fail(PINSAGE_EUNSUPPORTED, "num_groups %d above 4096", d->num_groups);
+  if ((d->num_groups > 0) != (d->offsets != nullptr))
+    return fail(PINSAGE_EINVAL, "offsets go with num_groups >= 1, and only with it");
+  if (n < 0) return fail(PINSAGE_EINVAL, "negative row count");
+  const int64_t wide = d->d_in > d->d_out ? d->d_in : d->d_out;
+  if (n >= (1ll << 31) ||
+      ((n + 63) / 64 + d->num_groups + 1) * ((wide + 63) / 64) >= (1ll << 31))
+    return fail(PINSAGE_EUNSUPPORTED, "%lld rows of %lld are too many for one call", (long long)n,
+                (long long)wide);
+  return PINSAGE_OK;
+}
+
+// Workspace of a backward pass: dz (where an activation makes it differ from
+// dy) | partial sums of db | partial sums of dW.
+struct DenseWs {
+  int64_t lddz = 0, piece = 0;
+  size_t dz = 0, db = 0, dw = 0;
+  size_t total() const { return dz + db + dw; }
+};
+
+DenseWs dense_ws(const pinsage_dense_t* d, int64_t n) {
+  DenseWs w;
+  w.lddz = (d->d_out + 7) / 8 * 8;
+  w.piece = dense_dw_piece(n, d->d_out, d->d_in, d->num_groups);
+  if (d->activation != PINSAGE_ACT_NONE) w.dz = align_up((size_t)n * w.lddz * elem_size(d->dtype));
+  w.db = align_up((size_t)dense_bias_pieces(n, d->num_groups) * d->d_out * 4);
+  w.dw = align_up((size_t)dense_dw_parts(n, w.piece, d->num_groups) * d->d_out * d->d_in * 4);
+  return w;
+}
+
+int check_newton(const pinsage_newton_schulz_t* p) {
+  if (!p) return fail(PINSAGE_EINVAL, "params are NULL");
+  if (p->dtype != PINSAGE_F32 && p->dtype != PINSAGE_BF16)
+    return fail(PINSAGE_EINVAL, "unknown dtype %d", (int)p->dtype);
+  if (p->batch < 0 || p->rows < 1 || p->cols < 1)
+    return fail(PINSAGE_EINVAL, "need batch >= 0 and rows, cols >= 1 (%lld, %d, %d)",
+                (long long)p->batch, p->rows, p->cols);
+  if (p->batch > 65535 || p->rows > 16384 || p->cols > 16384)
+    return fail(PINSAGE_EUNSUPPORTED, "batch above 65535 or a side above 16384");
+  if (p->steps < 1) return fail(PINSAGE_EINVAL, "steps must be >= 1");
+  if (p->steps > 64) return fail(PINSAGE_EUNSUPPORTED, "steps %d above 64", p->steps);
+  if (!(p->eps >= 0.0f) || !std::isfinite(p->eps) || !std::isfinite(p->a) ||
+      !std::isfinite(p->b) || !std::isfinite(p->c))
+    return fail(PINSAGE_EINVAL, "coefficients and eps must be finite, eps >= 0");
+  return PINSAGE_OK;
+}
+
+int check_workspace(const void* ws, size_t have, size_t need) {
+  if ((need > 0 && !ws) || have < need)
+    return fail(PINSAGE_EWORKSPACE, "workspace %zu bytes < required %zu", have, need);
+  if (reinterpret_cast<uintptr_t>(ws) % kAlign)
+    return fail(PINSAGE_EINVAL, "workspace is not 256-byte aligned");
+  return PINSAGE_OK;
+}
+
+NewtonLaunch newton_launch(const pinsage_newton_schulz_t* p, const void* in, void* out) {
+  NewtonLaunch a{};
+  a.in = in;
+  a.out = out;
+  a.batch = p->batch;
+  a.rows = p->rows;
+  a.cols = p->cols;
+  a.steps = p->steps;
+  a.a = p->a;
+  a.b = p->b;
+  a.c = p->c;
+  a.eps = p->eps;
+  a.bf16 = p->dtype == PINSAGE_BF16;
+  return a;
+}
+
+}  // namespace
+}  // namespace pinsage
+
+using namespace pinsage;
+
+extern "C" {
+
+int pinsage_dense_forward(const pinsage_dense_t* layer, const void* x, int64_t n, int64_t ldx,
+                          const void* residual, int64_t ldr, void* u, int64_t ldu, void* y,
+                          int64_t ldy, void* stream) {
+  g_last_error.clear();
+  int st = check_dense(layer, n);
+  if (st) return st;
+  if (n == 0) return PINSAGE_OK;
+  if (!x || !y || !layer->W) return fail(PINSAGE_EINVAL, "x, y or W is NULL");
+  if ((st = check_ld("x", ldx, layer->d_in)) || (st = check_ld("W", layer->ldw, layer->d_in)) ||
+      (st = check_ld("y", ldy, layer->d_out)) ||
+      (residual && (st = check_ld("residual", ldr, layer->d_out))) ||
+      (u && (st = check_ld("u", ldu, layer->d_out))))
+    return st;
+  DenseLaunch a{};
+  a.A = x;
+  a.lda = ldx;
+  a.B = layer->W;
+  a.ldb = layer->ldw;
+  a.group_stride = layer->d_out * layer->ldw;
+  a.bias = layer->b;
+  a.residual = residual;
+  a.ldr = ldr;
+  a.U = u;
+  a.ldu = ldu;
+  a.C = y;
+  a.ldc = ldy;
+  a.M = n;
+  a.N = layer->d_out;
+  a.K = layer->d_in;
+  a.offsets = layer->offsets;
+  a.G = layer->num_groups;
+  a.act = layer->activation;
+  a.bf16 = layer->dtype == PINSAGE_BF16;
+  const hipError_t e = launch_dense_rows(a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? PINSAGE_OK : hip_fail(e, "dense forward launch");
+}
+
+int pinsage_dense_backward_workspace_size(const pinsage_dense_t* layer, int64_t n, size_t* bytes) {
+  g_last_error.clear();
+  if (!bytes) return fail(PINSAGE_EINVAL, "bytes is NULL");
+  *bytes = 0;
+  const int st = check_dense(layer, n);
+  if (st) return st;
+  *bytes = dense_ws(layer, n).total();
+  return PINSAGE_OK;
+}
+
+int pinsage_dense_backward(const pinsage_dense_t* layer, const void* dy, int64_t lddy,
+                           const void* x, int64_t ldx, const void* u, int64_t ldu, int64_t n,
+                           void* dx, int64_t lddx, void* dW, float* db, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  g_last_error.clear();
+  int st = check_dense(layer, n);
+  if (st) return st;
+  const bool through = layer->activation != PINSAGE_ACT_NONE;
+  if (n > 0) {
+    if (!dy || (dW && !x) || (dx && !layer->W) || (through && !u))
+      return fail(PINSAGE_EINVAL, "dy, x, W or u is NULL where it is needed");
+    if ((st = check_ld("dy", lddy, layer->d_out)) ||
+        (dW && (st = check_ld("x", ldx, layer->d_in))) ||
+        (dx && ((st = check_ld("W", layer->ldw, layer->d_in)) ||
+                (st = check_ld("dx", lddx, layer->d_in)))) ||
+        (through && (st = check_ld("u", ldu, layer->d_out))))
+      return st;
+  }
+  const DenseWs w = dense_ws(layer, n);
+  if ((st = check_workspace(workspace, workspace_bytes, w.total()))) return st;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  unsigned char* const ws = static_cast<unsigned char*>(workspace);
+  DenseGradLaunch g{};
+  g.dy = dy;
+  g.lddy = lddy;
+  g.U = u;
+  g.ldu = ldu;
+  g.x = x;
+  g.ldx = ldx;
+  g.dz = through && (dx || dW) ? ws : nullptr;
+  g.lddz = w.lddz;
+  g.db = db;
+  g.db_parts = db ? reinterpret_cast<float*>(ws + w.dz) : nullptr;
+  g.dW = dW;
+  g.dw_parts = w.dw ? reinterpret_cast<float*>(ws + w.dz + w.db) : nullptr;
+  g.piece = (int)w.piece;
+  g.n = n;
+  g.N = layer->d_out;
+  g.K = layer->d_in;
+  g.offsets = layer->offsets;
+  g.G = layer->num_groups;
+  g.act = layer->activation;
+  g.bf16 = layer->dtype == PINSAGE_BF16;
+  hipError_t e;
+  if (g.dz || db) {
+    e = launch_dense_dz(g, s);
+    if (e != hipSuccess) return hip_fail(e, "dz launch");
+  }
+  if (!g.dz) {
+    g.dz = const_cast<void*>(dy);
+    g.lddz = lddy;
+  }
+  if (dx && n > 0) {
+    DenseLaunch a{};
+    a.A = g.dz;
+    a.lda = g.lddz;
+    a.B = layer->W;
+    a.ldb = layer->ldw;
+    a.group_stride = layer->d_out * layer->ldw;
+    a.b_col = true;
+    a.C = dx;
+    a.ldc = lddx;
+    a.M = n;
+    a.N = layer->d_in;
+    a.K = layer->d_out;
+    a.offsets = layer->offsets;
+    a.G = layer->num_groups;
+    a.act = kActNone;
+    a.bf16 = g.bf16;
+    e = launch_dense_rows(a, s);
+    if (e != hipSuccess) return hip_fail(e, "dx launch");
+  }
+  if (dW) {
+    e = launch_dense_dw(g, s);
+    if (e != hipSuccess) return hip_fail(e, "dW launch");
+  }
+  return PINSAGE_OK;
+}
+
+int pinsage_newton_schulz_workspace_size(const pinsage_newton_schulz_t* params, size_t* bytes) {
+  g_last_error.clear();
+  if (!bytes) return fail(PINSAGE_EINVAL, "bytes is NULL");
+  *bytes = 0;
+  const int st = check_newton(params);
+  if (st) return st;
+  *bytes = newton_workspace(params->batch, params->rows, params->cols,
+                            params->dtype == PINSAGE_BF16);
+  return PINSAGE_OK;
+}
+
+int pinsage_orthogonalize(const pinsage_newton_schulz_t* params, const void* in, void* out,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+  g_last_error.clear();
+  int st = check_newton(params);
+  if (st) return st;
+  if (params->batch == 0) return PINSAGE_OK;
+  if (!in || !out) return fail(PINSAGE_EINVAL, "in or out is NULL");
+  const NewtonLaunch a = newton_launch(params, in, out);
+  if ((st = check_workspace(workspace, workspace_bytes,
+                            newton_workspace(a.batch, a.rows, a.cols, a.bf16))))
+    return st;
+  const hipError_t e = launch_newton(a, workspace, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? PINSAGE_OK : hip_fail(e, "orthogonalisation launch");
+}
+
+int pinsage_muon_step(const pinsage_newton_schulz_t* params, const pinsage_muon_t* muon,
+                      const void* W, const void* grad, const float* momentum, void* W_out,
+                      float* momentum_out, void* workspace, size_t workspace_bytes, void* stream) {
+  g_last_error.clear();
+  int st = check_newton(params);
+  if (st) return st;
+  if (!muon) return fail(PINSAGE_EINVAL, "muon params are NULL");
+  if (!std::isfinite(muon->lr) || !std::isfinite(muon->beta) ||
+      !std::isfinite(muon->weight_decay) || !std::isfinite(muon->scale))
+    return fail(PINSAGE_EINVAL, "lr, beta, weight_decay and scale must be finite");
+  if (params->batch == 0) return PINSAGE_OK;
+  if (!W || !grad || !momentum || !W_out || !momentum_out)
+    return fail(PINSAGE_EINVAL, "a pointer argument is NULL");
+  NewtonLaunch a = newton_launch(params, grad, W_out);
+  a.weight = W;
+  a.momentum = momentum;
+  a.momentum_out = momentum_out;
+  a.beta = muon->beta;
+  a.decay = (float)(1.0 - (double)muon->lr * muon->weight_decay);
+  a.rate = muon->lr * muon->scale;
+  a.nesterov = muon->nesterov != 0;
+  if ((st = check_workspace(workspace, workspace_bytes,
+                            newton_workspace(a.batch, a.rows, a.cols, a.bf16))))
+    return st;
+  const hipError_t e = launch_newton(a, workspace, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? PINSAGE_OK : hip_fail(e, "optimiser step launch");
+}
+
+}  // extern "C"

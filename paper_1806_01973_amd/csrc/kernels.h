@@ -10,7 +10,8 @@ namespace pinsage {
 // Kernel classes for per-launch timing; values match PINSAGE_KERNEL_*.
 enum KernelClass { kKWalk = 0, kKGemmQ = 1, kKPool = 2, kKGemmW = 3, kKMinibatch = 4, kKLoss = 5,
                    kKGemmR = 6, kKMlp = 7, kKHardNeg = 8, kKGraphNbr = 9, kKGemmQR = 10,
-                   kKWalkTable = 11, kKPoolW = 12, kKCount = 13 };
+                   kKWalkTable = 11, kKPoolW = 12, kKDense = 13, kKDenseGrad = 14,
+                   kKNewtonSchulz = 15, kKCount = 16 };
 
 // Records a start/stop hipEvent pair around a launch when timing is enabled.
 class ProfileScope {
@@ -258,6 +259,100 @@ struct LossLaunch {
   float* loss;
 };
 hipError_t launch_loss(const LossLaunch& a, hipStream_t s);
+
+// Dense layers of the output head (dense.hip). Activations; values match
+// pinsage_activation_t.
+enum DenseAct { kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3 };
+
+// C[r][c] = act(U[r][c]) + residual[r][c], U[r][c] = sum_k A[r][k] B(c, k) + bias[c]
+// with B(c, k) = B[c * ldb + k], or B[k * ldb + c] when b_col, of row r's group:
+// group g holds rows offsets[g] .. offsets[g + 1] - 1 (device; null = one group) and
+// has B + g * group_stride, bias + g * N. Rows past the last group become zero.
+// Leading dimensions in elements; storage dtype bf16 or fp32, bias fp32.
+struct DenseLaunch {
+  const void* A;
+  int64_t lda;
+  const void* B;
+  int64_t ldb;
+  int64_t group_stride;
+  bool b_col;
+  const float* bias;     // nullable
+  const void* residual;  // nullable
+  int64_t ldr;
+  void* U;               // nullable
+  int64_t ldu;
+  void* C;
+  int64_t ldc;
+  int64_t M;
+  int N;
+  int K;
+  const int64_t* offsets;
+  int G;
+  int act;
+  bool bf16;
+};
+hipError_t launch_dense_rows(const DenseLaunch& a, hipStream_t s);
+
+// dz = dy * act'(U) and db (launch_dense_dz), dW[g] = dz^T x (launch_dense_dw) over
+// n rows of N outputs and K inputs. dz may be null (nothing written; dW then reads
+// dy as its dz, which the caller passes in `dz` of the second launch).
+constexpr int kBiasRows = 128;  // rows per partial sum of db
+struct DenseGradLaunch {
+  const void* dy;
+  int64_t lddy;
+  const void* U;
+  int64_t ldu;
+  const void* x;
+  int64_t ldx;
+  void* dz;
+  int64_t lddz;
+  float* db;        // nullable
+  float* db_parts;  // [dense_bias_pieces][N]; null when db is
+  void* dW;         // [G][N][K], dense
+  float* dw_parts;  // [dense_dw_parts][N][K]
+  int piece;        // rows per piece of dW's sums: dense_dw_piece
+  int64_t n;
+  int N;
+  int K;
+  const int64_t* offsets;
+  int G;
+  int act;
+  bool bf16;
+};
+__host__ __device__ inline int64_t dense_bias_pieces(int64_t n, int G) {
+  return (n + kBiasRows - 1) / kBiasRows + (G ? G + 1 : 0);
+}
+int64_t dense_dw_piece(int64_t n, int N, int K, int G);
+// Partial sums kept at most: only groups of two pieces or more keep any.
+__host__ __device__ inline int64_t dense_dw_parts(int64_t n, int64_t piece, int G) {
+  const int64_t pieces = (n + piece - 1) / piece;
+  return pieces < 2 ? 0 : (G ? 2 * pieces : pieces);
+}
+hipError_t launch_dense_dz(const DenseGradLaunch& a, hipStream_t s);
+hipError_t launch_dense_dw(const DenseGradLaunch& a, hipStream_t s);
+
+// Newton-Schulz orthogonalisation of `batch` matrices [rows][cols] (contiguous), and
+// the optimiser step around it (newton.hip). `update` null: X0 = in / (|in| + eps).
+struct NewtonLaunch {
+  const void* in;  // storage dtype
+  void* out;       // storage dtype: the result, or the new weight
+  int64_t batch;
+  int rows;
+  int cols;
+  int steps;
+  float a, b, c, eps;
+  bool bf16;
+  // The optimiser step (null `weight`: none): momentum' = beta momentum + in, the
+  // matrix orthogonalised is nesterov ? in + beta momentum' : momentum', and
+  // out = decay * weight - rate * result.
+  const void* weight = nullptr;
+  const float* momentum = nullptr;
+  float* momentum_out = nullptr;
+  float beta = 0, decay = 0, rate = 0;
+  bool nesterov = false;
+};
+size_t newton_workspace(int64_t batch, int rows, int cols, bool bf16);
+hipError_t launch_newton(const NewtonLaunch& a, void* workspace, hipStream_t s);
 
 // Frontier machinery of the minibatch forward (node flags + exclusive scan).
 hipError_t launch_fill_zero_u8(uint8_t* p, int64_t n, hipStream_t s);
