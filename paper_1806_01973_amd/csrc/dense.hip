@@ -5,16 +5,16 @@
 // (ragged: group g holds rows offsets[g] .. offsets[g + 1] - 1, read on the
 // device; empty groups allowed).
 //
-// The three products run on one tile core (product_device.h): the forward's
-// operands are both k-contiguous, dx reads W by columns, dW reads dz and x by
-// columns. dz is formed once, in the storage dtype (the products then read
+// The three products run on the same tile cores (ring_device.h where rows are whole
+// 16-byte vectors, else product_device.h): the forward's operands are both
+// k-contiguous, dx reads W by columns, dW reads dz and x by columns. dz is formed once, in the storage dtype (the products then read
 // 16-bit values; bf16 rounds it to 2^-9, which adds in quadrature to the same
 // rounding of dx and dW), by the kernel that also sums db, in fp32, from the
 // values before that rounding.
 #include <algorithm>
 
 #include "kernels.h"
-#include "product_device.h"
+#include "ring_device.h"
 
 namespace pinsage {
 namespace {
@@ -45,60 +45,6 @@ __device__ __forceinline__ float grad_through(float dy, float u, int act) {
     return dy * (s * (1.0f + u * (1.0f - s)));
   }
   return dy;
-}
-
-// ---- four elements of a row, any alignment -----------------------------------
-template <bool BF16>
-__device__ __forceinline__ void read4(const void* row, int64_t n, int cols, float (&v)[4]) {
-  if constexpr (BF16) {
-    const uint16_t* const p = static_cast<const uint16_t*>(row) + n;
-    if (cols >= 4) {
-      const uint2 w = load_any<uint2>(p);
-      v[0] = __uint_as_float(w.x << 16);
-      v[1] = __uint_as_float(w.x & 0xFFFF0000u);
-      v[2] = __uint_as_float(w.y << 16);
-      v[3] = __uint_as_float(w.y & 0xFFFF0000u);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = e < cols ? bf16_to_f32(p[e]) : 0.0f;
-    }
-  } else {
-    const float* const p = static_cast<const float*>(row) + n;
-    if (cols >= 4) {
-      const float4 w = load_any<float4>(p);
-      v[0] = w.x;
-      v[1] = w.y;
-      v[2] = w.z;
-      v[3] = w.w;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = e < cols ? p[e] : 0.0f;
-    }
-  }
-}
-
-template <bool BF16>
-__device__ __forceinline__ void write4(void* row, int64_t n, int cols, const float (&v)[4]) {
-  if constexpr (BF16) {
-    uint16_t* const p = static_cast<uint16_t*>(row) + n;
-    const uint2 w = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-    if (cols >= 4) {
-      store_any(p, w);
-    } else {
-      if (cols > 0) p[0] = (uint16_t)w.x;
-      if (cols > 1) p[1] = (uint16_t)(w.x >> 16);
-      if (cols > 2) p[2] = (uint16_t)w.y;
-    }
-  } else {
-    float* const p = static_cast<float*>(row) + n;
-    if (cols >= 4) {
-      store_any(p, make_float4(v[0], v[1], v[2], v[3]));
-    } else {
-#pragma unroll
-      for (int e = 0; e < 3; ++e)
-        if (e < cols) p[e] = v[e];
-    }
-  }
 }
 
 // ---- groups of rows ----------------------------------------------------------
@@ -205,16 +151,13 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void dense_rows_kernel(DenseLau
       static_cast<const unsigned char*>(a.B) + (int64_t)group * a.group_stride * C::ESZ;
   const bool orphans = a.offsets && group == a.G;  // rows of no group: zeros
 
-  f32x16 acc[C::TM][C::TN];
-  product_clear<C>(acc);
-  if (!orphans) {
-    const Operand A{Ap, a.lda, valid, 0};
-    const Operand B{Bg + (C::B_COL ? (int64_t)n0 : n0 * a.ldb) * C::ESZ, a.ldb,
-                    a.N - n0 < C::BN ? a.N - n0 : C::BN, 0};
-    product_tile<C>(A, B, 0, a.K, smem, acc);
-  }
+  TileSums<C> sums;
+  const Operand A{Ap, a.lda, valid, 0};
+  const Operand B{Bg + (C::B_COL ? (int64_t)n0 : n0 * a.ldb) * C::ESZ, a.ldb,
+                  a.N - n0 < C::BN ? a.N - n0 : C::BN, 0};
+  tile_sums(A, B, 0, orphans ? 0 : a.K, smem, sums);
   const float* const bias = a.bias && !orphans ? a.bias + (int64_t)group * a.N : nullptr;
-  product_rows<C>(acc, smem, [&](int m, int nn, float (&v)[4]) __attribute__((always_inline)) {
+  product_rows(sums, smem, [&](int m, int nn, float (&v)[4]) __attribute__((always_inline)) {
     const int n = n0 + nn;
     const int cols = a.N - n;
     if (m >= valid || cols <= 0) return;
@@ -382,7 +325,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void dense_few_kernel(DenseLaunch a
 }
 
 // ---- dz and db -----------------------------------------------------------------
-// A block takes a piece of kBiasRows rows of one group and up to 256 columns, a
+// A block takes a piece of a.bias_rows rows of one group and up to 256 columns, a
 // thread 4 columns of every (256 / lanes)-th row, lanes the smallest power of two
 // of threads that covers the columns.
 template <bool BF16>
@@ -392,7 +335,7 @@ __global__ __launch_bounds__(256) void dense_dz_kernel(DenseGradLaunch a, int la
   const int tid = threadIdx.x;
   Piece p;
   if (a.offsets) {
-    p = Groups{a.offsets, a.G, a.n, kBiasRows, true, true}.find(blockIdx.x, tid & 63);
+    p = Groups{a.offsets, a.G, a.n, a.bias_rows, true, true}.find(blockIdx.x, tid & 63);
     if (p.group < 0) return;
   } else {
     p.group = 0;
@@ -400,8 +343,8 @@ __global__ __launch_bounds__(256) void dense_dz_kernel(DenseGradLaunch a, int la
     p.hi = a.n;
     p.index = blockIdx.x;
   }
-  const int64_t r0 = p.lo + p.index * kBiasRows;
-  const int64_t r1 = p.hi - r0 < kBiasRows ? p.hi : r0 + kBiasRows;
+  const int64_t r0 = p.lo + p.index * a.bias_rows;
+  const int64_t r1 = p.hi - r0 < a.bias_rows ? p.hi : r0 + a.bias_rows;
   const int n = (blockIdx.y * lanes + tid % lanes) * 4, cols = a.N - n;
   float s[4] = {0, 0, 0, 0};
   if (cols > 0) {
@@ -442,16 +385,16 @@ __global__ __launch_bounds__(256) void dense_db_kernel(DenseGradLaunch a) {
   __shared__ float part[4][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int g = blockIdx.y, n = blockIdx.x * 64 + lane;
-  int64_t first = 0, pieces = (a.n + kBiasRows - 1) / kBiasRows;
+  int64_t first = 0, pieces = (a.n + a.bias_rows - 1) / a.bias_rows;
   if (a.offsets) {
-    const Groups gr{a.offsets, a.G, a.n, kBiasRows, true, true};
+    const Groups gr{a.offsets, a.G, a.n, a.bias_rows, true, true};
     int before = 0;
     for (int q = lane; q < g; q += 64) before += gr.pieces(q);
     first = wave_sum_i32(before);
     pieces = gr.pieces(g);
   }
   // Offsets that overlap could count more pieces than there are.
-  const int64_t all = dense_bias_pieces(a.n, a.offsets ? a.G : 0);
+  const int64_t all = dense_bias_pieces(a.n, a.offsets ? a.G : 0, a.bias_rows);
   if (first + pieces > all) pieces = first < all ? all - first : 0;
   const int64_t per = (pieces + 3) / 4;
   const int64_t q1 = per * (w + 1) < pieces ? per * (w + 1) : pieces;
@@ -502,15 +445,14 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void dense_dw_kernel(DenseGradL
       static_cast<const unsigned char*>(a.dz) + (r0 * a.lddz + n0) * C::ESZ;
   const unsigned char* const X =
       static_cast<const unsigned char*>(a.x) + (r0 * a.ldx + k0) * C::ESZ;
-  f32x16 acc[C::TM][C::TN];
-  product_clear<C>(acc);
-  product_tile<C>(Operand{Z, a.lddz, vn, 0}, Operand{X, a.ldx, vk, 0}, 0, rows, smem, acc);
+  TileSums<C> sums;
+  tile_sums(Operand{Z, a.lddz, vn, 0}, Operand{X, a.ldx, vk, 0}, 0, rows, smem, sums);
   // Offsets that overlap could count more pieces than the workspace holds.
   if (p.pieces > 1 && p.slot + p.index >= dense_dw_parts(a.n, a.piece, a.offsets ? a.G : 0)) return;
   float* const part = p.pieces > 1 ? a.dw_parts + (p.slot + p.index) * (int64_t)a.N * a.K : nullptr;
   unsigned char* const out =
       static_cast<unsigned char*>(a.dW) + (int64_t)p.group * a.N * a.K * C::ESZ;
-  product_rows<C>(acc, smem, [&](int m, int nn, float (&v)[4]) __attribute__((always_inline)) {
+  product_rows(sums, smem, [&](int m, int nn, float (&v)[4]) __attribute__((always_inline)) {
     const int cols = vk - nn;
     if (m >= vn || cols <= 0) return;
     if constexpr (!BF16)
@@ -561,22 +503,42 @@ __global__ __launch_bounds__(256) void dense_dw_join_kernel(DenseGradLaunch a) {
 }
 
 // ---- tile shapes -----------------------------------------------------------------
+// Ring: rows of whole 16-byte vectors; else the register core, which has no
+// 256 x 256 tile.
 template <bool BF16, bool A_COL, bool B_COL>
 struct Tiles;
 template <bool A_COL, bool B_COL>
 struct Tiles<true, A_COL, B_COL> {
+  using RingBig = RingCfg<kBf16, 256, 256, 64, 2, 4, A_COL, B_COL, 2>;
+  using RingMid = RingCfg<kBf16, 128, 128, 64, 2, 2, A_COL, B_COL, 2>;
+  using RingSmall = RingCfg<kBf16, 64, 64, 64, 2, 2, A_COL, B_COL, 4>;
   using Mid = ProductCfg<kBf16, 128, 128, 64, 2, 2, A_COL, B_COL, 2>;
   using Small = ProductCfg<kBf16, 64, 64, 128, 2, 2, A_COL, B_COL, 2>;
 };
 template <bool A_COL, bool B_COL>
 struct Tiles<false, A_COL, B_COL> {
+  using RingMid = RingCfg<kF32, 128, 128, 16, 2, 2, A_COL, B_COL, 4, 2>;
+  using RingSmall = RingCfg<kF32, 64, 64, 16, 2, 2, A_COL, B_COL, 4>;
+  using RingBig = RingMid;
   using Mid = ProductCfg<kF32, 128, 128, 32, 2, 2, A_COL, B_COL, 1>;
   using Small = ProductCfg<kF32, 64, 64, 64, 2, 2, A_COL, B_COL, 1>;
 };
 
+enum Shape { kSmall, kMid, kBig };
+constexpr int side(Shape s) { return s == kSmall ? 64 : (s == kMid ? 128 : 256); }
+
 inline int64_t tiles_of(int64_t m, int64_t n, int b) { return ((m + b - 1) / b) * ((n + b - 1) / b); }
 
-constexpr int64_t kFillTiles = 256;  // tiles of 128 below this leave CUs idle
+inline Shape rows_shape(int64_t m, int64_t n, bool bf16) {
+  if (!bf16) return tiles_of(m, n, 128) < 512 ? kSmall : kMid;
+  if (tiles_of(m, n, 64) <= 512) return kSmall;
+  return tiles_of(m, n, 256) < 256 ? kMid : kBig;
+}
+
+inline bool vectors(const void* p, int64_t ld, int64_t width, bool bf16) {
+  const int64_t ve = bf16 ? 8 : 4;
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % ve == 0 && width % ve == 0;
+}
 
 template <class C>
 hipError_t rows_cfg(const DenseLaunch& a, hipStream_t s) {
@@ -590,8 +552,20 @@ hipError_t rows_cfg(const DenseLaunch& a, hipStream_t s) {
 template <bool BF16, bool B_COL>
 hipError_t rows_dtype(const DenseLaunch& a, hipStream_t s) {
   using T = Tiles<BF16, false, B_COL>;
-  if (tiles_of(a.M, a.N, 128) < kFillTiles) return rows_cfg<typename T::Small>(a, s);
-  return rows_cfg<typename T::Mid>(a, s);
+  const Shape shape = rows_shape(a.M, a.N, BF16);
+  if (vectors(a.A, a.lda, a.K, BF16) && vectors(a.B, a.ldb, B_COL ? a.N : a.K, BF16)) {
+    if (shape == kSmall) return rows_cfg<typename T::RingSmall>(a, s);
+    if (shape == kMid) return rows_cfg<typename T::RingMid>(a, s);
+    return rows_cfg<typename T::RingBig>(a, s);
+  }
+  return shape == kSmall ? rows_cfg<typename T::Small>(a, s) : rows_cfg<typename T::Mid>(a, s);
+}
+
+// Tiles of dW: the largest of which enough pieces of 512 rows or more (1,024 under
+// 256 x 256) fill the chip.
+inline Shape dw_shape(int64_t n, int N, int K, bool bf16) {
+  if (bf16 && tiles_of(N, K, 256) * (n / 1024) >= 256 && N > 128 && K > 128) return kBig;
+  return tiles_of(N, K, 128) * (n / 512) >= 256 && N > 64 && K > 64 ? kMid : kSmall;
 }
 
 template <class C>
@@ -603,12 +577,21 @@ hipError_t dw_cfg(const DenseGradLaunch& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-bool dw_small(const DenseGradLaunch& a) { return tiles_of(a.N, a.K, 128) < 8; }
+template <bool BF16>
+hipError_t dw_tiles(const DenseGradLaunch& a, hipStream_t s) {
+  using T = Tiles<BF16, true, true>;
+  const Shape shape = dw_shape(a.n, a.N, a.K, BF16);
+  if (vectors(a.dz, a.lddz, a.N, BF16) && vectors(a.x, a.ldx, a.K, BF16)) {
+    if (shape == kSmall) return dw_cfg<typename T::RingSmall>(a, s);
+    if (shape == kMid) return dw_cfg<typename T::RingMid>(a, s);
+    return dw_cfg<typename T::RingBig>(a, s);
+  }
+  return shape == kSmall ? dw_cfg<typename T::Small>(a, s) : dw_cfg<typename T::Mid>(a, s);
+}
 
 template <bool BF16>
 hipError_t dw_dtype(const DenseGradLaunch& a, hipStream_t s) {
-  using T = Tiles<BF16, true, true>;
-  const hipError_t e = dw_small(a) ? dw_cfg<typename T::Small>(a, s) : dw_cfg<typename T::Mid>(a, s);
+  const hipError_t e = dw_tiles<BF16>(a, s);
   if (e != hipSuccess || !a.dw_parts) return e;
   const int64_t blocks = ((int64_t)a.N * a.K + 1023) / 1024;
   hipLaunchKernelGGL(dense_dw_join_kernel<BF16>, dim3((unsigned)blocks, a.offsets ? a.G : 1),
@@ -635,14 +618,12 @@ hipError_t launch_dense_rows(const DenseLaunch& a, hipStream_t s) {
   return a.bf16 ? rows_dtype<true, false>(a, s) : rows_dtype<false, false>(a, s);
 }
 
-// Rows per piece of dW's sums: as many pieces as give the chip two blocks per CU,
-// at least 256 rows each.
-int64_t dense_dw_piece(int64_t n, int N, int K, int G) {
-  const int64_t t128 = tiles_of(N, K, 128);
-  const int64_t tiles = (t128 < 8 ? tiles_of(N, K, 64) : t128) * (G ? G : 1);
-  const int64_t want = (512 + tiles - 1) / tiles * (G ? G : 1);
-  int64_t rows = (n + want - 1) / want;
-  rows = (rows + 63) / 64 * 64;
+// Rows per piece of dW's sums: as many pieces as give the chip 512 blocks, of 256
+// rows at least.
+int64_t dense_dw_piece(int64_t n, int N, int K, bool bf16) {
+  const int64_t tiles = tiles_of(N, K, side(dw_shape(n, N, K, bf16)));
+  const int64_t want = (512 + tiles - 1) / tiles;
+  const int64_t rows = ((n + want - 1) / want + 63) / 64 * 64;
   return rows < 256 ? 256 : rows;
 }
 
@@ -650,7 +631,7 @@ hipError_t launch_dense_dz(const DenseGradLaunch& a, hipStream_t s) {
   ProfileScope prof(kKDenseGrad, s);
   int lanes = 1;
   while (lanes < 64 && lanes * 4 < a.N) lanes *= 2;
-  const int64_t pieces = dense_bias_pieces(a.n, a.offsets ? a.G : 0);
+  const int64_t pieces = dense_bias_pieces(a.n, a.offsets ? a.G : 0, a.bias_rows);
   const dim3 grid((unsigned)(pieces > 0 ? pieces : 1), (unsigned)((a.N + 4 * lanes - 1) / (4 * lanes)));
   if (pieces > 0) {
     if (a.bf16) hipLaunchKernelGGL(dense_dz_kernel<true>, grid, dim3(256), 0, s, a, lanes);

@@ -296,7 +296,6 @@ hipError_t launch_dense_rows(const DenseLaunch& a, hipStream_t s);
 // dz = dy * act'(U) and db (launch_dense_dz), dW[g] = dz^T x (launch_dense_dw) over
 // n rows of N outputs and K inputs. dz may be null (nothing written; dW then reads
 // dy as its dz, which the caller passes in `dz` of the second launch).
-constexpr int kBiasRows = 128;  // rows per partial sum of db
 struct DenseGradLaunch {
   const void* dy;
   int64_t lddy;
@@ -308,6 +307,7 @@ struct DenseGradLaunch {
   int64_t lddz;
   float* db;        // nullable
   float* db_parts;  // [dense_bias_pieces][N]; null when db is
+  int bias_rows;    // rows per partial sum of db: dense_bias_rows
   void* dW;         // [G][N][K], dense
   float* dw_parts;  // [dense_dw_parts][N][K]
   int piece;        // rows per piece of dW's sums: dense_dw_piece
@@ -319,10 +319,15 @@ struct DenseGradLaunch {
   int act;
   bool bf16;
 };
-__host__ __device__ inline int64_t dense_bias_pieces(int64_t n, int G) {
-  return (n + kBiasRows - 1) / kBiasRows + (G ? G + 1 : 0);
+// 16 to 128, so that blocks of 256 columns make about 1,024.
+inline int dense_bias_rows(int64_t n, int N) {
+  const int64_t rows = n * ((N + 255) / 256) / 1024;
+  return rows >= 128 ? 128 : (rows >= 64 ? 64 : (rows >= 32 ? 32 : 16));
 }
-int64_t dense_dw_piece(int64_t n, int N, int K, int G);
+__host__ __device__ inline int64_t dense_bias_pieces(int64_t n, int G, int rows) {
+  return (n + rows - 1) / rows + (G ? G + 1 : 0);
+}
+int64_t dense_dw_piece(int64_t n, int N, int K, bool bf16);
 // Partial sums kept at most: only groups of two pieces or more keep any.
 __host__ __device__ inline int64_t dense_dw_parts(int64_t n, int64_t piece, int G) {
   const int64_t pieces = (n + piece - 1) / piece;

@@ -10,41 +10,29 @@
 // result rounds to bf16 once, at the end), fp32 storage as two (22 significand
 // bits, three MFMAs a product, against six for bf16 parts). Sums, and a X, run in
 // fp32; |G|_F is summed in fp64, so no finite G overflows.
-// X, A and B live in the workspace, padded with zeros to multiples of 128, so no
-// product has an edge. A and A A are symmetric: only their tiles on and above the
-// diagonal are computed, and stored twice.
+// X, its transpose T, A and B live in the workspace, padded with zeros to whole
+// tiles, so that no product has an edge and each reads both operands along k:
+// A = X X^T, A A^T, and B T^T. A and A A are symmetric: only their tiles on and
+// above the diagonal are computed, and stored twice.
 #include "kernels.h"
-#include "product_device.h"
+#include "ring_device.h"
 
 namespace pinsage {
 namespace {
 
 constexpr float kScale = 4096.0f;  // the stored values over the true ones
-constexpr int kPad = 128;
-constexpr int kNormBlocks = 64;    // partial sums of a matrix's norm
-
-inline int padded(int v) { return (v + kPad - 1) / kPad * kPad; }
+constexpr int kMaxNormBlocks = 256;  // partial sums of a matrix's norm
 
 struct NewtonWork {
-  double* norms;     // [batch][kNormBlocks]
+  double* norms;     // [batch][kMaxNormBlocks]
   uint16_t* X[2];    // [batch][planes][mp][np]
+  uint16_t* T[2];    // [batch][planes][np][mp]
   uint16_t* A;       // [batch][planes][mp][mp]
   uint16_t* B;
   int m, n, mp, np;  // m <= n; padded
+  int norm_blocks;
   bool flip;         // X is G^T
 };
-
-// ---- four elements of the storage dtype, any alignment -------------------------
-template <bool BF16>
-__device__ __forceinline__ float read1(const void* p, int64_t at) {
-  if constexpr (BF16) return bf16_to_f32(static_cast<const uint16_t*>(p)[at]);
-  else return static_cast<const float*>(p)[at];
-}
-template <bool BF16>
-__device__ __forceinline__ void write1(void* p, int64_t at, float v) {
-  if constexpr (BF16) static_cast<uint16_t*>(p)[at] = f32_to_bf16(v);
-  else static_cast<float*>(p)[at] = v;
-}
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
@@ -54,16 +42,19 @@ __device__ __forceinline__ float unpack_f16(uint32_t w, int h) {
   return (float)__builtin_bit_cast(f16x2, w)[h];
 }
 
-// Stores four scaled values as one or two fp16 parts; p on 8 bytes.
-template <int PLANES>
-__device__ __forceinline__ void put4(uint16_t* p, int64_t plane, const float (&v)[4]) {
-  const uint2 hi = make_uint2(pack_f16(v[0], v[1]), pack_f16(v[2], v[3]));
-  *reinterpret_cast<uint2*>(p) = hi;
-  if constexpr (PLANES == 2) {
-    const uint2 lo = make_uint2(pack_f16(v[0] - unpack_f16(hi.x, 0), v[1] - unpack_f16(hi.x, 1)),
-                                pack_f16(v[2] - unpack_f16(hi.y, 0), v[3] - unpack_f16(hi.y, 1)));
-    *reinterpret_cast<uint2*>(p + plane) = lo;
+// Stores N scaled values as one or two fp16 parts; p on 2 N bytes.
+template <int PLANES, int N>
+__device__ __forceinline__ void put(uint16_t* p, int64_t plane, const float (&v)[N]) {
+  typedef uint32_t words __attribute__((ext_vector_type(N / 2)));
+  words hi, lo;
+#pragma unroll
+  for (int e = 0; e < N / 2; ++e) {
+    hi[e] = pack_f16(v[2 * e], v[2 * e + 1]);
+    if constexpr (PLANES == 2)
+      lo[e] = pack_f16(v[2 * e] - unpack_f16(hi[e], 0), v[2 * e + 1] - unpack_f16(hi[e], 1));
   }
+  *reinterpret_cast<words*>(p) = hi;
+  if constexpr (PLANES == 2) *reinterpret_cast<words*>(p + plane) = lo;
 }
 template <int PLANES>
 __device__ __forceinline__ void get4(const uint16_t* p, int64_t plane, float (&v)[4]) {
@@ -82,13 +73,16 @@ __device__ __forceinline__ void get4(const uint16_t* p, int64_t plane, float (&v
 }
 
 // ---- the norm, with the momentum's update ---------------------------------------
-// What is orthogonalised: the input, or the step's combination of it with the
-// already updated momentum.
+// What is orthogonalised, elements at .. at + 3 of the batch's storage: the input,
+// or the step's combination of it with the already updated momentum.
 template <bool BF16>
-__device__ __forceinline__ float update_at(const NewtonLaunch& a, int64_t at, float momentum) {
-  const float g = read1<BF16>(a.in, at);
-  if (!a.weight) return g;
-  return a.nesterov ? fmaf(a.beta, momentum, g) : momentum;
+__device__ __forceinline__ void update4(const NewtonLaunch& a, int64_t at, int cols, float (&u)[4]) {
+  read4<BF16>(a.in, at, cols, u);
+  if (!a.weight) return;
+  float m[4];
+  read4<false>(a.momentum_out, at, cols, m);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) u[e] = a.nesterov ? fmaf(a.beta, m[e], u[e]) : m[e];
 }
 
 template <bool BF16>
@@ -96,64 +90,88 @@ __global__ __launch_bounds__(256) void newton_norm_kernel(NewtonLaunch a, Newton
   __shared__ double part[4];
   const int64_t size = (int64_t)a.rows * a.cols, base = blockIdx.y * size;
   double s = 0.0;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += kNormBlocks * 256) {
-    float mom = 0.0f;
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < size;
+       i += (int64_t)w.norm_blocks * 1024) {
+    const int cols = (int)(size - i < 4 ? size - i : 4);
+    float u[4];
     if (a.weight) {
-      mom = fmaf(a.beta, a.momentum[base + i], read1<BF16>(a.in, base + i));
-      a.momentum_out[base + i] = mom;
+      float m[4];
+      read4<BF16>(a.in, base + i, cols, u);
+      read4<false>(a.momentum, base + i, cols, m);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        m[e] = fmaf(a.beta, m[e], u[e]);
+        u[e] = a.nesterov ? fmaf(a.beta, m[e], u[e]) : m[e];
+      }
+      write4<false>(a.momentum_out, base + i, cols, m);
+    } else {
+      read4<BF16>(a.in, base + i, cols, u);
     }
-    const double u = update_at<BF16>(a, base + i, mom);
-    s = fma(u, u, s);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s = fma((double)u[e], (double)u[e], s);
   }
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
   __syncthreads();
   if (threadIdx.x == 0)
-    w.norms[blockIdx.y * kNormBlocks + blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
+    w.norms[blockIdx.y * kMaxNormBlocks + blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// ---- X0: scaled, split into fp16 parts, transposed when flipped, padded ----------
+// ---- X0 and its transpose: scaled, in fp16 parts, padded --------------------------
 template <bool BF16>
 __global__ __launch_bounds__(256) void newton_start_kernel(NewtonLaunch a, NewtonWork w) {
   constexpr int PLANES = BF16 ? 1 : 2;
   __shared__ float tile[64][65];
-  const int tid = threadIdx.x, lane = tid & 63;
-  double s = w.norms[(int64_t)blockIdx.z * kNormBlocks + lane];
+  __shared__ double part[4];
+  const int tid = threadIdx.x;
+  double s = tid < w.norm_blocks ? w.norms[(int64_t)blockIdx.z * kMaxNormBlocks + tid] : 0.0;
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o);
+  if ((tid & 63) == 0) part[tid >> 6] = s;
+  __syncthreads();
+  s = (part[0] + part[1]) + (part[2] + part[3]);
   const double inv = (double)kScale / (sqrt(s) + (double)a.eps);
   const int64_t base = (int64_t)blockIdx.z * a.rows * a.cols;
-  const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;  // in X
-  for (int q = tid >> 6; q < 64; q += 4) {
-    // Along G's rows, so that reads are contiguous either way.
-    const int gr = w.flip ? j0 + q : i0 + q, gc = w.flip ? i0 + lane : j0 + lane;
-    float v = 0.0f;
-    if (gr < a.rows && gc < a.cols) {
-      const int64_t at = base + (int64_t)gr * a.cols + gc;
-      v = (float)(update_at<BF16>(a, at, a.weight ? a.momentum_out[at] : 0.0f) * inv);
-    }
-    if (w.flip) tile[lane][q] = v;
-    else tile[q][lane] = v;
+  const int r0 = (w.flip ? blockIdx.x : blockIdx.y) * 64;  // of G
+  const int c0 = (w.flip ? blockIdx.y : blockIdx.x) * 64;
+#pragma unroll
+  for (int q = tid; q < 64 * 16; q += 256) {
+    const int r = q / 16, c = q % 16 * 4, cols = a.cols - c0 - c;
+    float u[4] = {0, 0, 0, 0};
+    if (r0 + r < a.rows && cols > 0)
+      update4<BF16>(a, base + (int64_t)(r0 + r) * a.cols + c0 + c, cols, u);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) tile[r][c + e] = (float)(u[e] * inv);
   }
   __syncthreads();
+  // The tile as it lies goes to X, or to T when X is G^T; turned, to the other.
   const int64_t plane = (int64_t)w.mp * w.np;
-  uint16_t* const X = w.X[0] + blockIdx.z * PLANES * plane;
-  for (int q = tid; q < 64 * 16; q += 256) {
-    const int i = q / 16, j = q % 16 * 4;
-    const float v[4] = {tile[i][j], tile[i][j + 1], tile[i][j + 2], tile[i][j + 3]};
-    put4<PLANES>(X + (int64_t)(i0 + i) * w.np + j0 + j, plane, v);
+  uint16_t* const along = (w.flip ? w.T[0] : w.X[0]) + blockIdx.z * PLANES * plane;
+  uint16_t* const across = (w.flip ? w.X[0] : w.T[0]) + blockIdx.z * PLANES * plane;
+  const int64_t lda = w.flip ? w.mp : w.np, ldx = w.flip ? w.np : w.mp;
+#pragma unroll
+  for (int q = tid; q < 64 * 8; q += 256) {
+    const int i = q / 8, j = q % 8 * 8;
+    float v[8], t[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = tile[i][j + e];
+      t[e] = tile[j + e][i];
+    }
+    put<PLANES>(along + (int64_t)(r0 + i) * lda + c0 + j, plane, v);
+    put<PLANES>(across + (int64_t)(c0 + i) * ldx + r0 + j, plane, t);
   }
 }
 
 // ---- the three products -----------------------------------------------------------
 enum NewtonProduct { kGram = 0, kSquare = 1, kApply = 2, kLast = 3 };
 
-// P[i][j] = sum_k L(i, k) R(j, k): X X^T, A A (A is symmetric), or B X.
+// P[i][j] = sum_k L[i][k] R[j][k]: X X^T, A A (A is symmetric), or B X = B (X^T)^T.
 template <class C, int KIND, bool BF16>
 __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch a, NewtonWork w,
                                                                     int from) {
-  __shared__ __attribute__((aligned(16))) unsigned char smem[C::LDS_BYTES];
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[C::LDS_BYTES];
   constexpr int PLANES = C::MEM_PLANES;
   constexpr bool kSymmetric = KIND == kGram || KIND == kSquare;
   const int64_t px = (int64_t)w.mp * w.np, pa = (int64_t)w.mp * w.mp, z = blockIdx.y;
@@ -174,8 +192,6 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch
     tj = blockIdx.x % T;
   }
   const int i0 = ti * C::BM, j0 = tj * C::BN;
-  f32x16 acc[C::TM][C::TN];
-  product_clear<C>(acc);
   Operand L, R;
   int depth;
   if constexpr (KIND == kGram) {
@@ -188,86 +204,125 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch
     depth = w.mp;
   } else {
     L = Operand{B + (int64_t)i0 * w.mp, w.mp, C::BM, pa * 2};
-    R = Operand{X + j0, w.np, C::BN, px * 2};
+    R = Operand{w.T[from] + z * PLANES * px + (int64_t)j0 * w.mp, w.mp, C::BN, px * 2};
     depth = w.mp;
   }
-  product_tile<C>(L, R, 0, depth, smem, acc);
+  TileSums<C> sums;
+  tile_sums(L, R, 0, depth, smem, sums);
 
   // Products carry the scale twice.
   const float back = 1.0f / kScale;
   if constexpr (kSymmetric) {
     uint16_t* const out = KIND == kGram ? A : B;
-    const bool mirror = ti != tj;
-    product_rows<C>(acc, smem, [&](int m, int n, float (&v)[4]) __attribute__((always_inline)) {
-      const int64_t at = (int64_t)(i0 + m) * w.mp + j0 + n;
-      if constexpr (KIND == kGram) {
+    product_rows_cols(
+        sums, smem,
+        [&](int m, int n, float (&v)[4]) __attribute__((always_inline)) {
+          const int64_t at = (int64_t)(i0 + m) * w.mp + j0 + n;
+          if constexpr (KIND == kGram) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] *= back;
-      } else {
-        float x[4];
-        get4<PLANES>(A + at, pa, x);
+            for (int e = 0; e < 4; ++e) v[e] *= back;
+          } else {
+            float x[4];
+            get4<PLANES>(A + at, pa, x);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = fmaf(a.b, x[e], a.c * back * v[e]);
-      }
-      put4<PLANES>(out + at, pa, v);
-      if (mirror) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int64_t to = (int64_t)(j0 + n + e) * w.mp + i0 + m;
-          const _Float16 hi = (_Float16)v[e];
-          out[to] = __builtin_bit_cast(uint16_t, hi);
-          if constexpr (PLANES == 2)
-            out[pa + to] = __builtin_bit_cast(uint16_t, (_Float16)(v[e] - (float)hi));
-        }
-      }
-    });
+            for (int e = 0; e < 4; ++e) v[e] = fmaf(a.b, x[e], a.c * back * v[e]);
+          }
+          put<PLANES>(out + at, pa, v);
+        },
+        [&](int m, int n, const float (&v)[8]) __attribute__((always_inline)) {
+          put<PLANES>(out + (int64_t)(j0 + n) * w.mp + i0 + m, pa, v);
+        },
+        ti != tj);
   } else if constexpr (KIND == kApply) {
-    uint16_t* const out = w.X[1 - from] + z * PLANES * px;
-    product_rows<C>(acc, smem, [&](int m, int n, float (&v)[4]) __attribute__((always_inline)) {
-      const int64_t at = (int64_t)(i0 + m) * w.np + j0 + n;
-      float x[4];
-      get4<PLANES>(X + at, px, x);
+    uint16_t* const outx = w.X[1 - from] + z * PLANES * px;
+    uint16_t* const outt = w.T[1 - from] + z * PLANES * px;
+    product_rows_cols(
+        sums, smem,
+        [&](int m, int n, float (&v)[4]) __attribute__((always_inline)) {
+          const int64_t at = (int64_t)(i0 + m) * w.np + j0 + n;
+          float x[4];
+          get4<PLANES>(X + at, px, x);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = fmaf(a.a, x[e], back * v[e]);
-      put4<PLANES>(out + at, px, v);
-    });
+          for (int e = 0; e < 4; ++e) v[e] = fmaf(a.a, x[e], back * v[e]);
+          put<PLANES>(outx + at, px, v);
+        },
+        [&](int m, int n, const float (&v)[8]) __attribute__((always_inline)) {
+          put<PLANES>(outt + (int64_t)(j0 + n) * w.mp + i0 + m, px, v);
+        },
+        true);
   } else {
     const int64_t base = z * a.rows * a.cols;
-    product_rows<C>(acc, smem, [&](int m, int n, float (&v)[4]) __attribute__((always_inline)) {
-      const int i = i0 + m, j = j0 + n;
-      if (i >= w.m || j >= w.n) return;
-      float x[4];
-      get4<PLANES>(X + (int64_t)i * w.np + j, px, x);
+    // Up to four results of one row of G, from `at` on.
+    auto give = [&](int64_t at, int cols, float (&y)[4]) __attribute__((always_inline)) {
+      if (a.weight) {
+        float old[4];
+        read4<BF16>(a.weight, at, cols, old);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (j + e >= w.n) break;
-        const int64_t at = base + (w.flip ? (int64_t)(j + e) * a.cols + i : (int64_t)i * a.cols + j + e);
-        float y = fmaf(a.a, x[e], back * v[e]) * back;
-        if (a.weight) y = fmaf(a.decay, read1<BF16>(a.weight, at), -a.rate * y);
-        write1<BF16>(a.out, at, y);
+        for (int e = 0; e < 4; ++e) y[e] = fmaf(a.decay, old[e], -a.rate * y[e]);
       }
-    });
+      write4<BF16>(a.out, at, cols, y);
+    };
+    product_rows_cols(
+        sums, smem,
+        [&](int m, int n, float (&v)[4]) __attribute__((always_inline)) {
+          const int i = i0 + m, j = j0 + n;
+          float x[4];
+          get4<PLANES>(X + (int64_t)i * w.np + j, px, x);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = fmaf(a.a, x[e], back * v[e]) * back;
+          if (!w.flip && i < w.m && j < w.n) give(base + (int64_t)i * a.cols + j, w.n - j, v);
+        },
+        [&](int m, int n, const float (&v)[8]) __attribute__((always_inline)) {
+          const int i = i0 + m, j = j0 + n;
+          if (j >= w.n) return;
+#pragma unroll
+          for (int h = 0; h < 8; h += 4) {
+            float y[4] = {v[h], v[h + 1], v[h + 2], v[h + 3]};
+            if (i + h < w.m) give(base + (int64_t)j * a.cols + i + h, w.m - i - h, y);
+          }
+        },
+        w.flip);
   }
 }
 
-template <class CR, class CC, bool BF16>
-hipError_t iterate(const NewtonLaunch& a, const NewtonWork& w, hipStream_t s) {
-  const int T = w.mp / CR::BM, TX = T * (w.np / CC::BN), batch = (int)a.batch;
-  int from = 0;
-  for (int k = 0; k < a.steps; ++k) {
-    hipLaunchKernelGGL((newton_kernel<CR, kGram, BF16>), dim3(T * (T + 1) / 2, batch),
-                       dim3(CR::THREADS), 0, s, a, w, from);
-    hipLaunchKernelGGL((newton_kernel<CR, kSquare, BF16>), dim3(T * (T + 1) / 2, batch),
-                       dim3(CR::THREADS), 0, s, a, w, from);
-    if (k + 1 < a.steps)
-      hipLaunchKernelGGL((newton_kernel<CC, kApply, BF16>), dim3(TX, batch), dim3(CC::THREADS), 0, s,
-                         a, w, from);
+// ---- tile shapes --------------------------------------------------------------------
+// Small tiles as long as all run at once, two blocks per CU: fp16, K = 2,048, 512 tiles
+// of 64 x 64 17.0 us against 19.9 for 128 of 128 x 128 and 1,024 37.0 against 24.1;
+// two parts 59.5 against 57.0 us at 1,024 tiles of 64 x 64. Of the fp16 128 x 128 tiles
+// the ring of four stages while there is one tile per CU (24.9 against 26.1 us), else
+// two blocks of two stages.
+inline int64_t tiles_of(const NewtonWork& w, int64_t batch, bool symmetric, int side) {
+  const int64_t tm = (w.mp + side - 1) / side, tn = (w.np + side - 1) / side;
+  return (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batch;
+}
+inline bool small_tiles(const NewtonWork& w, int64_t batch, bool symmetric, bool bf16) {
+  return tiles_of(w, batch, symmetric, 64) <= (bf16 ? 576 : 1024);
+}
+
+template <class C, int KIND, bool BF16>
+void launch_one(const NewtonLaunch& a, const NewtonWork& w, int from, hipStream_t s) {
+  const int64_t tiles = tiles_of(w, 1, KIND == kGram || KIND == kSquare, C::BM);
+  hipLaunchKernelGGL((newton_kernel<C, KIND, BF16>), dim3((unsigned)tiles, (unsigned)a.batch),
+                     dim3(C::THREADS), 0, s, a, w, from);
+}
+
+template <int KIND, bool BF16>
+void launch_product(const NewtonLaunch& a, const NewtonWork& w, int from, hipStream_t s) {
+  constexpr bool kSymmetric = KIND == kGram || KIND == kSquare;
+  const bool small = small_tiles(w, a.batch, kSymmetric, BF16);
+  if constexpr (BF16) {
+    if (small)
+      launch_one<RingCfg<kF16, 64, 64, 64, 2, 2, false, false, 4>, KIND, true>(a, w, from, s);
+    else if (tiles_of(w, a.batch, kSymmetric, 128) <= 256)
+      launch_one<RingCfg<kF16, 128, 128, 64, 2, 2, false, false, 4>, KIND, true>(a, w, from, s);
     else
-      hipLaunchKernelGGL((newton_kernel<CC, kLast, BF16>), dim3(TX, batch), dim3(CC::THREADS), 0, s,
-                         a, w, from);
-    from = 1 - from;
+      launch_one<RingCfg<kF16, 128, 128, 64, 2, 2, false, false, 2>, KIND, true>(a, w, from, s);
+  } else {
+    if (small)
+      launch_one<RingCfg<kF16x2, 64, 64, 64, 2, 2, false, false, 2>, KIND, false>(a, w, from, s);
+    else
+      launch_one<RingCfg<kF16x2, 128, 128, 32, 2, 2, false, false, 4>, KIND, false>(a, w, from, s);
   }
-  return hipGetLastError();
 }
 
 inline size_t aligned(size_t v) { return (v + 255) / 256 * 256; }
@@ -276,35 +331,43 @@ size_t layout(int64_t batch, int rows, int cols, bool bf16, unsigned char* ws, N
   w->flip = rows > cols;
   w->m = w->flip ? cols : rows;
   w->n = w->flip ? rows : cols;
-  w->mp = padded(w->m);
-  w->np = padded(w->n);
+  w->mp = (w->m + 63) / 64 * 64;
+  w->np = (w->n + 63) / 64 * 64;
+  if (!small_tiles(*w, batch, true, bf16) || !small_tiles(*w, batch, false, bf16)) {
+    w->mp = (w->m + 127) / 128 * 128;
+    w->np = (w->n + 127) / 128 * 128;
+  }
+  const int64_t blocks = ((int64_t)rows * cols + 4095) / 4096;
+  w->norm_blocks = (int)(blocks < kMaxNormBlocks ? blocks : kMaxNormBlocks);
   const size_t planes = bf16 ? 1 : 2;
   const size_t x = aligned((size_t)batch * planes * w->mp * w->np * 2);
   const size_t g = aligned((size_t)batch * planes * w->mp * w->mp * 2);
-  const size_t norms = aligned((size_t)batch * kNormBlocks * sizeof(double));
+  const size_t norms = aligned((size_t)batch * kMaxNormBlocks * sizeof(double));
   w->norms = reinterpret_cast<double*>(ws);
-  w->X[0] = reinterpret_cast<uint16_t*>(ws + norms);
-  w->X[1] = reinterpret_cast<uint16_t*>(ws + norms + x);
-  w->A = reinterpret_cast<uint16_t*>(ws + norms + 2 * x);
-  w->B = reinterpret_cast<uint16_t*>(ws + norms + 2 * x + g);
-  return norms + 2 * x + 2 * g;
+  uint16_t* const rest = reinterpret_cast<uint16_t*>(ws + norms);
+  w->X[0] = rest;
+  w->X[1] = rest + x / 2;
+  w->T[0] = rest + x;
+  w->T[1] = rest + x / 2 * 3;
+  w->A = rest + x * 2;
+  w->B = rest + x * 2 + g / 2;
+  return norms + 4 * x + 2 * g;
 }
 
 template <bool BF16>
 hipError_t launch_dtype(const NewtonLaunch& a, const NewtonWork& w, hipStream_t s) {
-  constexpr int MODE = BF16 ? kF16 : kF16x2;
-  hipLaunchKernelGGL(newton_norm_kernel<BF16>, dim3(kNormBlocks, (unsigned)a.batch), dim3(256), 0, s,
+  const unsigned batch = (unsigned)a.batch;
+  hipLaunchKernelGGL(newton_norm_kernel<BF16>, dim3((unsigned)w.norm_blocks, batch), dim3(256), 0, s,
                      a, w);
   hipLaunchKernelGGL(newton_start_kernel<BF16>,
-                     dim3((unsigned)(w.np / 64), (unsigned)(w.mp / 64), (unsigned)a.batch), dim3(256),
-                     0, s, a, w);
-  constexpr int BK = BF16 ? 64 : 32;
-  const int64_t tiles = (int64_t)(w.mp / 128) * (w.np / 128) * a.batch;
-  if (tiles >= 256)
-    return iterate<ProductCfg<MODE, 128, 128, BK, 2, 2, false, false, 2>,
-                   ProductCfg<MODE, 128, 128, BK, 2, 2, false, true, 2>, BF16>(a, w, s);
-  return iterate<ProductCfg<MODE, 64, 64, 2 * BK, 2, 2, false, false, 2>,
-                 ProductCfg<MODE, 64, 64, 2 * BK, 2, 2, false, true, 2>, BF16>(a, w, s);
+                     dim3((unsigned)(w.np / 64), (unsigned)(w.mp / 64), batch), dim3(256), 0, s, a, w);
+  for (int k = 0, from = 0; k < a.steps; ++k, from = 1 - from) {
+    launch_product<kGram, BF16>(a, w, from, s);
+    launch_product<kSquare, BF16>(a, w, from, s);
+    if (k + 1 < a.steps) launch_product<kApply, BF16>(a, w, from, s);
+    else launch_product<kLast, BF16>(a, w, from, s);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace

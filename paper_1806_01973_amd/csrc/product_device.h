@@ -88,6 +88,60 @@ __device__ __forceinline__ void store_any(void* p, const T& v) {
   __builtin_memcpy(p, &v, sizeof(T));
 }
 
+// Four elements of a row from column n on, `cols` of which exist; any alignment.
+template <bool BF16>
+__device__ __forceinline__ void read4(const void* row, int64_t n, int cols, float (&v)[4]) {
+  if constexpr (BF16) {
+    const uint16_t* const p = static_cast<const uint16_t*>(row) + n;
+    if (cols >= 4) {
+      const uint2 w = load_any<uint2>(p);
+      v[0] = __uint_as_float(w.x << 16);
+      v[1] = __uint_as_float(w.x & 0xFFFF0000u);
+      v[2] = __uint_as_float(w.y << 16);
+      v[3] = __uint_as_float(w.y & 0xFFFF0000u);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = e < cols ? bf16_to_f32(p[e]) : 0.0f;
+    }
+  } else {
+    const float* const p = static_cast<const float*>(row) + n;
+    if (cols >= 4) {
+      const float4 w = load_any<float4>(p);
+      v[0] = w.x;
+      v[1] = w.y;
+      v[2] = w.z;
+      v[3] = w.w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = e < cols ? p[e] : 0.0f;
+    }
+  }
+}
+
+template <bool BF16>
+__device__ __forceinline__ void write4(void* row, int64_t n, int cols, const float (&v)[4]) {
+  if constexpr (BF16) {
+    uint16_t* const p = static_cast<uint16_t*>(row) + n;
+    const uint2 w = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    if (cols >= 4) {
+      store_any(p, w);
+    } else {
+      if (cols > 0) p[0] = (uint16_t)w.x;
+      if (cols > 1) p[1] = (uint16_t)(w.x >> 16);
+      if (cols > 2) p[2] = (uint16_t)w.y;
+    }
+  } else {
+    float* const p = static_cast<float*>(row) + n;
+    if (cols >= 4) {
+      store_any(p, make_float4(v[0], v[1], v[2], v[3]));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (e < cols) p[e] = v[e];
+    }
+  }
+}
+
 template <int BK>
 __device__ __forceinline__ int product_swizzle(int row) {
   return BK == 32 ? ((row >> 1) ^ (row >> 3)) & 3 : (row ^ (row >> 3)) & 7;
@@ -119,18 +173,36 @@ __device__ __forceinline__ u32x4 load_part(const unsigned char* p, int count) {
   return v;
 }
 
-// acc[i][j] += the tile's products over k in [k0, k1): the 32 x 32 block i, j of
-// this wave, of which a lane holds row lane % 32 and columns 8 (e / 4) +
-// 4 (lane / 32) + e % 4. All of the block's threads call it; smem holds
-// C::LDS_BYTES and is free again when it returns (after a barrier).
+// A wave's blocks of 32 x 32 sums: block i, j has its rows from
+// row0 + 32 i and its columns from col0 + 32 j of the tile, of which a lane holds
+// row lane % 32 and columns 8 (e / 4) + 4 (lane / 32) + e % 4.
+template <class C>
+struct TileSums {
+  f32x16 v[C::TM][C::TN];
+  int row0, col0;
+};
+
+__device__ __forceinline__ void clear_block(f32x16& v) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) v[e] = 0.0f;
+}
+
+// The tile's products over k in [k0, k1). All of the block's threads call it; smem
+// holds C::LDS_BYTES and is free again when it returns (after a barrier).
 template <class C>
 __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B, int64_t k0,
-                                             int64_t k1, unsigned char* smem,
-                                             f32x16 (&acc)[C::TM][C::TN]) {
+                                             int64_t k1, unsigned char* smem, TileSums<C>& sums) {
+  auto& acc = sums.v;
+#pragma unroll
+  for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j) clear_block(acc[i][j]);
   constexpr int BK = C::BK, ESZ = C::ESZ, VE = C::VE, T = C::LOADERS, PL = C::PLANES;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / C::WAVES_N, wn = wave % C::WAVES_N;
+  sums.row0 = wm * C::WM;
+  sums.col0 = wn * C::WN;
   const bool is_a = wave < C::NWAVES / 2;
   const int t = is_a ? tid : tid - T;
   const unsigned char* const src = static_cast<const unsigned char*>(is_a ? A.p : B.p);
@@ -322,47 +394,60 @@ __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B,
   }
 }
 
-template <class C>
-__device__ __forceinline__ void product_clear(f32x16 (&acc)[C::TM][C::TN]) {
-#pragma unroll
-  for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-    for (int j = 0; j < C::TN; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-}
-
 // Hands the tile out in whole rows: f(m, n, v) with the tile's row m and its
-// columns n .. n + 3, a wave's lanes side by side along the columns. A wave's
-// bands of 32 rows pass through LDS of its own.
-template <class C, class F>
-__device__ __forceinline__ void product_rows(const f32x16 (&acc)[C::TM][C::TN],
-                                             unsigned char* smem, F f) {
+// columns n .. n + 3, a wave's lanes side by side along the columns, then, when
+// `turned`, by columns: g(m, n, v) with rows m .. m + 7 of column n, of the values
+// that f left in v. A wave's bands of 32 rows pass through LDS of its own.
+template <class C, class F, class G>
+__device__ __forceinline__ void product_rows_cols(const TileSums<C>& sums, unsigned char* smem, F f,
+                                                  G g, bool turned) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int wm = wave / C::WAVES_N, wn = wave % C::WAVES_N;
   float* const stage = reinterpret_cast<float*>(smem + wave * C::STAGE_BYTES);
-  constexpr int LANES = C::WN / 4;  // per row
+  constexpr int WIDTH = C::WN, LANES = WIDTH / 4;  // per row
 #pragma unroll
   for (int i = 0; i < C::TM; ++i) {
 #pragma unroll
     for (int j = 0; j < C::TN; ++j)
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<float4*>(stage + (lane & 31) * C::STAGE_LD + 32 * j + 8 * g +
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4*>(stage + (lane & 31) * C::STAGE_LD + 32 * j + 8 * q +
                                    4 * (lane >> 5)) =
-            make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
-                        acc[i][j][4 * g + 3]);
+            make_float4(sums.v[i][j][4 * q], sums.v[i][j][4 * q + 1], sums.v[i][j][4 * q + 2],
+                        sums.v[i][j][4 * q + 3]);
     wave_lds_sync();
+    const int m0 = sums.row0 + 32 * i;
 #pragma unroll
     for (int r0 = 0; r0 < 32; r0 += 64 / LANES) {
       const int r = r0 + lane / LANES, col = lane % LANES * 4;
-      const float4 x = *reinterpret_cast<const float4*>(stage + r * C::STAGE_LD + col);
+      float4* const at = reinterpret_cast<float4*>(stage + r * C::STAGE_LD + col);
+      const float4 x = *at;
       float v[4] = {x.x, x.y, x.z, x.w};
-      f(wm * C::WM + 32 * i + r, wn * C::WN + col, v);
+      f(m0 + r, sums.col0 + col, v);
+      if (turned) *at = make_float4(v[0], v[1], v[2], v[3]);
     }
     wave_lds_sync();
+    if (turned) {
+      constexpr int PER = 64 / WIDTH > 0 ? 64 / WIDTH : 1;  // groups of eight rows at once
+#pragma unroll
+      for (int c0 = 0; c0 < WIDTH; c0 += 64)
+#pragma unroll
+        for (int r0 = 0; r0 < 32; r0 += 8 * PER) {
+          const int n = c0 + lane % (WIDTH < 64 ? WIDTH : 64);
+          const int r = r0 + 8 * (lane / (WIDTH < 64 ? WIDTH : 64));
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = stage[(r + e) * C::STAGE_LD + n];
+          g(m0 + r, sums.col0 + n, v);
+        }
+      wave_lds_sync();
+    }
   }
+}
+
+template <class C, class F>
+__device__ __forceinline__ void product_rows(const TileSums<C>& sums, unsigned char* smem, F f) {
+  product_rows_cols(sums, smem, f, [](int, int, const float (&)[8]) {}, false);
 }
 
 // Elements of a row's four that a split product left without a finite value,

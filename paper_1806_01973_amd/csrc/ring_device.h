@@ -1,0 +1,370 @@
+// The tile product of product_device.h for operands whose rows are whole 16-byte
+// vectors, fed by DMA.
+//
+// Chunks of BK columns of k travel global -> LDS directly (no registers, no
+// VALU beside one scalar add per chunk) into a ring of STAGES stages, up to
+// STAGES chunks ahead of the MFMAs, with one barrier per chunk: the register
+// path has one chunk in flight, and where a CU holds one tile a chunk's MFMAs
+// (0.2 us at 128 x 128 x 64) are far shorter than a load's latency.
+// A row operand lies in LDS as rows of BK values, 16-byte slot v of row r at
+// v ^ swizzle(r); a column operand as it lies in memory, BK rows of BM values. Of
+// 16-bit values its fragments come through the transposing LDS read (16 lanes read
+// four k rows of 16 m; lane i gets the four k of m = i), slot s of row k at
+// s ^ ring_col_swizzle(k); of fp32 as eight 4-byte reads.
+// fp32 values are split into their three bf16 parts after the LDS read, among the
+// MFMAs of the step before: 7 VALU instructions a value, twice per value and tile
+// with 64 x 64 wave tiles, under 6 MFMAs per product.
+//
+// What bounds it is the LDS: at 128 bytes a clock, the fragments of a 64 x 64 wave
+// tile (4 KB for 4 MFMAs of 32 clocks on each of 4 SIMDs) and the DMA's writes
+// take longer than the MFMAs of a 128 x 128 tile, as long as those of 256 x 256
+// (wave tiles of 128 x 64); and a CU's loads, 64 bytes a clock, as long as the
+// MFMAs of 128 x 128. Waves that share a tile's k steps, so that smaller tiles keep
+// larger wave tiles, gained 5% at most and are not here.
+// Where rows end inside a tile, lanes read the last row or vector again (the
+// results of those rows are never used); past the end of k they read zeros.
+#pragma once
+
+#include <type_traits>
+
+#include "product_device.h"
+
+namespace pinsage {
+
+__device__ __attribute__((aligned(16))) const uint32_t g_ring_zero[4] = {0, 0, 0, 0};
+
+template <int MODE_, int BM_, int BN_, int BK_, int WAVES_M_, int WAVES_N_, bool A_COL_,
+          bool B_COL_, int STAGES_, int WPE_ = 1>
+struct RingCfg {
+  static constexpr int MODE = MODE_, BM = BM_, BN = BN_, BK = BK_, STAGES = STAGES_, WPE = WPE_;
+  static constexpr int WAVES_M = WAVES_M_, WAVES_N = WAVES_N_;
+  static constexpr bool A_COL = A_COL_, B_COL = B_COL_;
+  static constexpr int NWAVES = WAVES_M * WAVES_N, THREADS = 64 * NWAVES;
+  static constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, TM = WM / 32, TN = WN / 32;
+  static constexpr int ESZ = MODE == kF32 ? 4 : 2, MEM_PLANES = MODE == kF16x2 ? 2 : 1;
+  static constexpr int PARTS = MODE == kF32 ? 3 : MEM_PLANES;  // of a fragment
+  static constexpr int A_PLANE = BM * BK * ESZ, B_PLANE = BN * BK * ESZ;
+  static constexpr int BUF_BYTES = (A_PLANE + B_PLANE) * MEM_PLANES;
+  static constexpr int STEPS = BK / 16;  // k steps of a chunk
+  // One DMA instruction of a wave fills a group of 1 KB.
+  static constexpr int A_GROUPS = A_PLANE / 1024, B_GROUPS = B_PLANE / 1024;  // per plane
+  static constexpr int DA = A_GROUPS * MEM_PLANES / NWAVES;  // of a wave, per chunk
+  static constexpr int DB = B_GROUPS * MEM_PLANES / NWAVES;
+  static constexpr int PENDING = (STAGES - 2) * (DA + DB);
+  static constexpr int STAGE_LD = WN + 4;
+  static constexpr int STAGE_BYTES = 32 * STAGE_LD * 4;
+  static constexpr int RING = STAGES * BUF_BYTES;
+  static constexpr int LDS_BYTES = RING > NWAVES * STAGE_BYTES ? RING : NWAVES * STAGE_BYTES;
+  static_assert(A_GROUPS * MEM_PLANES % NWAVES == 0 && B_GROUPS * MEM_PLANES % NWAVES == 0 &&
+                    A_GROUPS % DA == 0 && B_GROUPS % DB == 0,
+                "every wave serves one plane of each operand");
+  static_assert(STAGES >= 2 && PENDING <= 63 && LDS_BYTES <= 160 * 1024, "");
+  static_assert(BK * ESZ == 64 || BK * ESZ == 128, "rows of 4 or 8 slots");
+};
+
+// Slot swizzle of a row operand of `SLOTS` 16-byte slots a row.
+template <int SLOTS>
+__device__ __forceinline__ int ring_row_swizzle(int r) {
+  return product_swizzle<SLOTS * 8>(r);
+}
+__device__ __forceinline__ int ring_col_swizzle(int k) { return (k & 3) << 1; }
+
+__device__ __forceinline__ void ring_dma(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(lds), "v"(off), "s"(base)
+               : "memory");
+}
+__device__ __forceinline__ void ring_dma_at(const void* p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :
+               : "s"(lds), "v"(p)
+               : "memory");
+}
+template <int N>
+__device__ __forceinline__ void ring_wait() {
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+__device__ __forceinline__ void ring_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+}
+
+// A pointer that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ const unsigned char* ring_uniform(const unsigned char* p) {
+  const uint64_t v = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return reinterpret_cast<const unsigned char*>(((uint64_t)hi << 32) | lo);
+}
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// As product_tile; operands' `p` and `ld` multiples of 16 bytes, and so the
+// `valid` values of a column operand and the k1 - k0 of a row operand.
+template <class C>
+__device__ __forceinline__ void ring_tile(const Operand& A, const Operand& B, int64_t k0,
+                                          int64_t k1, unsigned char* smem, TileSums<C>& sums) {
+  constexpr int BK = C::BK, ESZ = C::ESZ, VE = 16 / ESZ, STAGES = C::STAGES;
+  constexpr int PARTS = C::PARTS, PLANES = C::MEM_PLANES, SLOTS = BK / VE;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int wm = wave / C::WAVES_N, wn = wave % C::WAVES_N;
+  sums.row0 = wm * C::WM;
+  sums.col0 = wn * C::WN;
+  auto& acc = sums.v;
+#pragma unroll
+  for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j) clear_block(acc[i][j]);
+  const int nchunks = __builtin_amdgcn_readfirstlane((int)((k1 - k0 + BK - 1) / BK));
+  if (nchunks <= 0) return;
+  const uint32_t smem_base =
+      (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
+
+  // ---- this wave's DMAs --------------------------------------------------------
+  constexpr int DA = C::DA, DB = C::DB;
+  const int first_a = wave * DA, first_b = wave * DB;  // its groups of a stage
+  const unsigned char* base_a =
+      static_cast<const unsigned char*>(A.p) + first_a / C::A_GROUPS * A.plane;
+  const unsigned char* base_b =
+      static_cast<const unsigned char*>(B.p) + first_b / C::B_GROUPS * B.plane;
+  uint32_t off[DA + DB];  // from the chunk's base
+  int kk[DA + DB];        // the vector's first k within the chunk
+  auto place = [&](auto column, int d, int g, int width, const Operand& o)
+      __attribute__((always_inline)) {
+    if constexpr (decltype(column)::value) {
+      const int spr = width / VE, k = g * 64 / spr + lane / spr;
+      int m = ((lane % spr) ^ (ESZ == 2 ? ring_col_swizzle(k) : 0)) * VE;
+      m = m < o.valid ? m : o.valid - VE;
+      off[d] = ((uint32_t)k * (uint32_t)o.ld + (uint32_t)m) * ESZ;
+      kk[d] = k;
+    } else {
+      const int r = g * (64 / SLOTS) + lane / SLOTS;
+      const int v = (lane % SLOTS) ^ ring_row_swizzle<SLOTS>(r);
+      off[d] = ((uint32_t)(r < o.valid ? r : o.valid - 1) * (uint32_t)o.ld + (uint32_t)(v * VE)) * ESZ;
+      kk[d] = v * VE;
+    }
+  };
+#pragma unroll
+  for (int d = 0; d < DA; ++d)
+    place(std::bool_constant<C::A_COL>{}, d, first_a % C::A_GROUPS + d, C::BM, A);
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+    place(std::bool_constant<C::B_COL>{}, DA + d, first_b % C::B_GROUPS + d, C::BN, B);
+  const int64_t step_a = (C::A_COL ? A.ld * BK : BK) * ESZ;
+  const int64_t step_b = (C::B_COL ? B.ld * BK : BK) * ESZ;
+  base_a = ring_uniform(base_a + (C::A_COL ? k0 * A.ld : k0) * ESZ);
+  base_b = ring_uniform(base_b + (C::B_COL ? k0 * B.ld : k0) * ESZ);
+  const int whole = __builtin_amdgcn_readfirstlane((int)((k1 - k0) / BK));  // chunks inside k
+  const int rest = (int)((k1 - k0) % BK);
+  auto issue = [&](int c) __attribute__((always_inline)) {
+    const uint32_t dst = smem_base + (uint32_t)((c % STAGES) * C::BUF_BYTES);
+    const uint32_t dst_a = dst + first_a * 1024;
+    const uint32_t dst_b = dst + PLANES * C::A_PLANE + first_b * 1024;
+    if (c < whole) {
+#pragma unroll
+      for (int d = 0; d < DA; ++d)
+        ring_dma(base_a, off[d], __builtin_amdgcn_readfirstlane(dst_a + d * 1024));
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+        ring_dma(base_b, off[DA + d], __builtin_amdgcn_readfirstlane(dst_b + d * 1024));
+      base_a += step_a;
+      base_b += step_b;
+    } else {
+      // The last part of k, or beyond it: groups of zeros keep the count of loads in
+      // flight the same.
+      const int left = c == whole ? rest : 0;
+      const unsigned char* const zero = reinterpret_cast<const unsigned char*>(g_ring_zero);
+#pragma unroll
+      for (int d = 0; d < DA; ++d)
+        ring_dma_at(kk[d] < left ? base_a + off[d] : zero,
+                    __builtin_amdgcn_readfirstlane(dst_a + d * 1024));
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+        ring_dma_at(kk[DA + d] < left ? base_b + off[DA + d] : zero,
+                    __builtin_amdgcn_readfirstlane(dst_b + d * 1024));
+    }
+  };
+
+  // ---- fragments ------------------------------------------------------------------
+  const int frag_row = lane & 31, half = lane >> 5;
+  struct Frags {
+    u32x4 a[C::TM][PARTS], b[C::TN][PARTS];
+  };
+  // Eight k of one row: a vector of 16-bit values, or two of fp32 (in parts 0 and 1).
+  auto read_row = [&](const unsigned char* tile, int r, int ks, u32x4 (&out)[PARTS])
+      __attribute__((always_inline)) {
+    const unsigned char* const row = tile + r * (BK * ESZ);
+    const int s0 = (2 * ks + half) * (8 / VE), sw = ring_row_swizzle<SLOTS>(r);
+    out[0] = *reinterpret_cast<const u32x4*>(row + (s0 ^ sw) * 16);
+    if constexpr (ESZ == 4) out[1] = *reinterpret_cast<const u32x4*>(row + ((s0 + 1) ^ sw) * 16);
+  };
+  // The same of a column operand: with 16-bit values a lane (j, c) of 16 reads k row
+  // j's values 4 c .. 4 c + 3, twice for k and k + 4.
+  auto read_col = [&](const unsigned char* tile, int m0, int ks, int width, u32x4 (&out)[PARTS])
+      __attribute__((always_inline)) {
+    if constexpr (ESZ == 4) {
+      const unsigned char* const at =
+          tile + ((16 * ks + 8 * half) * width + m0 + frag_row) * 4;
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        out[k >> 2][k & 3] = *reinterpret_cast<const uint32_t*>(at + k * width * 4);
+    } else {
+      const int m = m0 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int k = 16 * ks + 8 * half + 4 * h + ((lane >> 2) & 3);
+        const unsigned char* const at =
+            tile + k * (width * 2) + (((m >> 3) ^ ring_col_swizzle(k)) * 16) + (m & 4) * 2;
+        const s16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4*)at);
+        const u32x2 x = __builtin_bit_cast(u32x2, w);
+        out[0][2 * h] = x[0];
+        out[0][2 * h + 1] = x[1];
+      }
+    }
+  };
+  // Step ks of chunk c.
+  auto read = [&](int c, int ks, Frags& f) __attribute__((always_inline)) {
+    const unsigned char* const a0 = smem + (c % STAGES) * C::BUF_BYTES;
+    const unsigned char* const b0 = a0 + PLANES * C::A_PLANE;
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i) {
+      const int m = wm * C::WM + 32 * i;
+      if constexpr (PLANES == 2) {
+        u32x4 x[PARTS];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          if constexpr (C::A_COL) read_col(a0 + p * C::A_PLANE, m, ks, C::BM, x);
+          else read_row(a0 + p * C::A_PLANE, m + frag_row, ks, x);
+          f.a[i][p] = x[0];
+        }
+      } else if constexpr (C::A_COL) {
+        read_col(a0, m, ks, C::BM, f.a[i]);
+      } else {
+        read_row(a0, m + frag_row, ks, f.a[i]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j) {
+      const int n = wn * C::WN + 32 * j;
+      if constexpr (PLANES == 2) {
+        u32x4 x[PARTS];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          if constexpr (C::B_COL) read_col(b0 + p * C::B_PLANE, n, ks, C::BN, x);
+          else read_row(b0 + p * C::B_PLANE, n + frag_row, ks, x);
+          f.b[j][p] = x[0];
+        }
+      } else if constexpr (C::B_COL) {
+        read_col(b0, n, ks, C::BN, f.b[j]);
+      } else {
+        read_row(b0, n + frag_row, ks, f.b[j]);
+      }
+    }
+  };
+  auto split = [&](Frags& f) __attribute__((always_inline)) {
+    if constexpr (ESZ == 4) {
+      uint32_t key = 0;
+#pragma unroll
+      for (int i = 0; i < C::TM; ++i) {
+        const Split3 s = split3(f.a[i][0], f.a[i][1], key);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) f.a[i][p] = s.p[p];
+      }
+#pragma unroll
+      for (int j = 0; j < C::TN; ++j) {
+        const Split3 s = split3(f.b[j][0], f.b[j][1], key);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) f.b[j][p] = s.p[p];
+      }
+    }
+  };
+  auto multiply = [&](const Frags& f) __attribute__((always_inline)) {
+    constexpr int PRODUCTS = PARTS * (PARTS + 1) / 2;
+#pragma unroll
+    for (int q = 0; q < PRODUCTS; ++q) {
+      constexpr int kB3[6] = {2, 0, 1, 1, 0, 0}, kA3[6] = {0, 2, 1, 0, 1, 0};
+      const int pb = kB3[6 - PRODUCTS + q], pa = kA3[6 - PRODUCTS + q];
+#pragma unroll
+      for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j)
+          acc[i][j] = product_mfma<C::MODE>(f.b[j][pb], f.a[i][pa], acc[i][j]);
+    }
+  };
+  // The products of a step, and the splitting of the next one's values among them.
+  auto work = [&](const Frags& cur, Frags& nxt) __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_barrier(0);
+    split(nxt);
+    multiply(cur);
+    if constexpr (ESZ == 4) {
+      constexpr int kMfma = 6 * C::TM * C::TN, kValu = 56 * (C::TM + C::TN);
+#pragma unroll
+      for (int q = 0; q < kMfma; ++q) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                            // MFMA
+        __builtin_amdgcn_sched_group_barrier(0x002, (kValu + kMfma - 1) / kMfma, 0);  // VALU
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // Chunks 0 .. STAGES - 1 go out; a chunk is waited for (STAGES - 2 younger ones may
+  // stay in flight) and the barrier shows everybody's and frees the chunk before,
+  // whose stage takes chunk c + STAGES. The last step's MFMAs of a chunk follow that
+  // barrier, over the first fragment reads of the next.
+#pragma unroll
+  for (int c = 0; c < STAGES - 1; ++c) issue(c);
+  ring_wait<C::PENDING>();
+  ring_barrier();
+  issue(STAGES - 1);
+  Frags f[2];
+  read(0, 0, f[0]);
+  split(f[0]);
+  auto chunk = [&](int c, auto parity) __attribute__((always_inline)) {
+    constexpr int P = decltype(parity)::value;
+#pragma unroll
+    for (int s = 0; s + 1 < C::STEPS; ++s) {
+      read(c, s + 1, f[(P + s + 1) & 1]);
+      work(f[(P + s) & 1], f[(P + s + 1) & 1]);
+    }
+    ring_wait<C::PENDING>();
+    ring_barrier();
+    Frags& nxt = f[(P + C::STEPS) & 1];
+    read(c + 1, 0, nxt);  // past the last chunk: zeros, unused
+    __builtin_amdgcn_sched_barrier(0);
+    issue(c + STAGES);
+    work(f[(P + C::STEPS - 1) & 1], nxt);
+  };
+  using Even = std::integral_constant<int, 0>;
+  using Odd = std::integral_constant<int, 1>;
+  int c = 0;
+  if constexpr (C::STEPS % 2) {
+    for (; c + 1 < nchunks; c += 2) {
+      chunk(c, Even{});
+      chunk(c + 1, Odd{});
+    }
+    if (c < nchunks) chunk(c, Even{});
+  } else {
+    for (; c < nchunks; ++c) chunk(c, Even{});
+  }
+  ring_wait<0>();
+  __syncthreads();
+}
+
+// The tile product a configuration stands for.
+template <int M, int BM, int BN, int BK, int WM, int WN, bool AC, bool BC, int NB, int E>
+__device__ __forceinline__ void tile_sums(
+    const Operand& A, const Operand& B, int64_t k0, int64_t k1, unsigned char* smem,
+    TileSums<ProductCfg<M, BM, BN, BK, WM, WN, AC, BC, NB, E>>& sums) {
+  product_tile(A, B, k0, k1, smem, sums);
+}
+template <int M, int BM, int BN, int BK, int WM, int WN, bool AC, bool BC, int S, int E>
+__device__ __forceinline__ void tile_sums(
+    const Operand& A, const Operand& B, int64_t k0, int64_t k1, unsigned char* smem,
+    TileSums<RingCfg<M, BM, BN, BK, WM, WN, AC, BC, S, E>>& sums) {
+  ring_tile(A, B, k0, k1, smem, sums);
+}
+
+}  // namespace pinsage
