@@ -1904,31 +1904,30 @@ int pinsage_dense_backward(const pinsage_dense_t* layer, const void* dy, int64_t
     g.dz = const_cast<void*>(dy);
     g.lddz = lddy;
   }
-  if (dx && n > 0) {
-    DenseLaunch a{};
-    a.A = g.dz;
-    a.lda = g.lddz;
-    a.B = layer->W;
-    a.ldb = layer->ldw;
-    a.group_stride = layer->d_out * layer->ldw;
-    a.b_col = true;
-    a.C = dx;
-    a.ldc = lddx;
-    a.M = n;
-    a.N = layer->d_in;
-    a.K = layer->d_out;
-    a.offsets = layer->offsets;
-    a.G = layer->num_groups;
-    a.act = kActNone;
-    a.bf16 = g.bf16;
-    e = launch_dense_rows(a, s);
-    if (e != hipSuccess) return hip_fail(e, "dx launch");
-  }
-  if (dW) {
-    e = launch_dense_dw(g, s);
-    if (e != hipSuccess) return hip_fail(e, "dW launch");
-  }
-  return PINSAGE_OK;
+  DenseLaunch a{};
+  a.A = g.dz;
+  a.lda = g.lddz;
+  a.B = layer->W;
+  a.ldb = layer->ldw;
+  a.group_stride = layer->d_out * layer->ldw;
+  a.b_col = true;
+  a.C = dx;
+  a.ldc = lddx;
+  a.M = n;
+  a.N = layer->d_in;
+  a.K = layer->d_out;
+  a.offsets = layer->offsets;
+  a.G = layer->num_groups;
+  a.act = kActNone;
+  a.bf16 = g.bf16;
+  const bool rows = dx && n > 0;
+  if (rows && dW) e = launch_dense_dx_dw(a, g, s);
+  else if (rows) e = launch_dense_rows(a, s);
+  else if (dW) e = launch_dense_dw(g, s);
+  else e = hipSuccess;
+  if (e != hipSuccess) return hip_fail(e, "dx and dW launch");
+  e = launch_dense_join(g, s);
+  return e == hipSuccess ? PINSAGE_OK : hip_fail(e, "gradient sums launch");
 }
 
 int pinsage_newton_schulz_workspace_size(const pinsage_newton_schulz_t* params, size_t* bytes) {

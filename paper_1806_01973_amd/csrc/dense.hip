@@ -86,34 +86,64 @@ struct Groups {
     const int p = (int)((hi - lo + unit - 1) / unit);
     return at_least_one && p == 0 ? 1 : p;
   }
-  // All lanes of a wave take part in these two; the results are wave-uniform.
-  __device__ __forceinline__ int total(int lane) const {
-    int sum = 0;
-    for (int g0 = 0; g0 < count(); g0 += 64)
-      sum += g0 + lane < count() ? pieces(g0 + lane) : 0;
-    return wave_sum_i32(sum);
-  }
-  __device__ __forceinline__ Piece find(int t, int lane) const {
+  // Piece t, or, given `tiles` per piece, the piece and tile (in t) of block
+  // `block` in an order that keeps neighbouring tiles on one XCD. All lanes of a wave
+  // take part; the results are wave-uniform. Up to 64 groups the offsets are read once.
+  __device__ __forceinline__ Piece find(int lane, int& t, int block, int tiles) const {
     Piece out;
+    const int all = count();
+    int64_t lo = 0, hi = 0;
+    int p = 0;
+    auto load = [&](int g) __attribute__((always_inline)) {
+      lo = hi = 0;
+      if (g < all) bounds(g, lo, hi);
+      const int q = (int)((hi - lo + unit - 1) / unit);
+      p = g < all ? (at_least_one && q == 0 ? 1 : q) : 0;
+    };
+    load(lane);
+    int incl = wave_inclusive_sum(p, lane);
+    if (tiles > 0) {
+      int total = __builtin_amdgcn_readlane(incl, 63);
+      for (int g0 = 64; g0 < all; g0 += 64) {
+        load(g0 + lane);
+        total += wave_sum_i32(p);
+      }
+      if (all > 64) {
+        load(lane);
+        incl = wave_inclusive_sum(p, lane);
+      }
+      total *= tiles;
+      if (block >= total) return out;
+      const int at = xcd_tile(block, total);
+      t = at % tiles;
+      tiles = at / tiles;  // the piece
+    } else {
+      tiles = t;
+    }
     int before = 0, slots = 0;
-    for (int g0 = 0; g0 < count(); g0 += 64) {
-      const int p = g0 + lane < count() ? pieces(g0 + lane) : 0;
-      const int incl = wave_inclusive_sum(p, lane) + before;
+    for (int g0 = 0;;) {
       const int slot_incl = wave_inclusive_sum(p > 1 ? p : 0, lane) + slots;
-      const unsigned long long past = __ballot(incl > t);
+      incl += before;
+      const unsigned long long past = __ballot(incl > tiles);
       if (past) {
         const int l = __builtin_ctzll(past);
         out.group = g0 + l;
         out.pieces = __builtin_amdgcn_readlane(p, l);
-        out.index = t - (__builtin_amdgcn_readlane(incl, l) - out.pieces);
+        out.index = tiles - (__builtin_amdgcn_readlane(incl, l) - out.pieces);
         out.slot = __builtin_amdgcn_readlane(slot_incl, l) - (out.pieces > 1 ? out.pieces : 0);
-        bounds(out.group, out.lo, out.hi);
+        out.lo = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(lo >> 32), l) << 32) |
+                           (uint32_t)__builtin_amdgcn_readlane((int)lo, l));
+        out.hi = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(hi >> 32), l) << 32) |
+                           (uint32_t)__builtin_amdgcn_readlane((int)hi, l));
         return out;
       }
       before = __builtin_amdgcn_readlane(incl, 63);
       slots = __builtin_amdgcn_readlane(slot_incl, 63);
+      g0 += 64;
+      if (g0 >= all) return out;
+      load(g0 + lane);
+      incl = wave_inclusive_sum(p, lane);
     }
-    return out;
   }
 };
 
@@ -121,70 +151,85 @@ struct Groups {
 // C[r][c] = act(sum_k A[r][k] B(c, k) + bias[c]) + residual[r][c], U[r][c] the
 // value before act. B(c, k) = B[c * ldb + k] (B_COL: B[k * ldb + c]) of r's group.
 template <class C>
-__global__ __launch_bounds__(C::THREADS, C::WPE) void dense_rows_kernel(DenseLaunch a) {
-  __shared__ __attribute__((aligned(16))) unsigned char smem[C::LDS_BYTES];
+__device__ __forceinline__ void rows_block(const DenseLaunch& a, int block, int blocks,
+                                           unsigned char* smem) {
   constexpr bool BF16 = C::MODE == kBf16;
   const int lane = threadIdx.x & 63;
   const int tiles_n = (a.N + C::BN - 1) / C::BN;
-  int tile;
-  int64_t lo = 0, hi = a.M, m0;
-  int group = 0;
+  int64_t hi = a.M, m0;
+  int group = 0, tile_n = 0;
   if (a.offsets) {
-    const Groups gr{a.offsets, a.G, a.M, C::BM, false, true};
-    const int total = gr.total(lane) * tiles_n;
-    if ((int)blockIdx.x >= total) return;
-    tile = xcd_tile(blockIdx.x, total);
-    const Piece p = gr.find(tile / tiles_n, lane);
+    const Piece p = Groups{a.offsets, a.G, a.M, C::BM, false, true}.find(lane, tile_n, block, tiles_n);
     if (p.group < 0) return;
     group = p.group;
-    lo = p.lo;
     hi = p.hi;
-    m0 = lo + p.index * C::BM;
+    m0 = p.lo + p.index * C::BM;
   } else {
-    tile = xcd_tile(blockIdx.x, gridDim.x);
+    const int tile = xcd_tile(block, blocks);
     m0 = (int64_t)(tile / tiles_n) * C::BM;
+    tile_n = tile % tiles_n;
   }
-  const int n0 = (tile % tiles_n) * C::BN;
+  const int n0 = tile_n * C::BN;
   const int valid = (int)(hi - m0 < C::BM ? hi - m0 : C::BM);
   const unsigned char* const Ap = static_cast<const unsigned char*>(a.A) + m0 * a.lda * C::ESZ;
   const unsigned char* const Bg =
       static_cast<const unsigned char*>(a.B) + (int64_t)group * a.group_stride * C::ESZ;
   const bool orphans = a.offsets && group == a.G;  // rows of no group: zeros
 
+  // A lane keeps its columns through the epilogue: the bias is read once, ahead.
+  constexpr int V = BF16 ? 8 : 4;
+  float bias[V] = {};
+  const int lane_n = n0 + product_column<C, V>();
+  if (a.bias && !orphans && lane_n < a.N)
+    read_row<false>(a.bias + (int64_t)group * a.N, lane_n, a.N - lane_n, bias);
+
   TileSums<C> sums;
   const Operand A{Ap, a.lda, valid, 0};
   const Operand B{Bg + (C::B_COL ? (int64_t)n0 : n0 * a.ldb) * C::ESZ, a.ldb,
                   a.N - n0 < C::BN ? a.N - n0 : C::BN, 0};
   tile_sums(A, B, 0, orphans ? 0 : a.K, smem, sums);
-  const float* const bias = a.bias && !orphans ? a.bias + (int64_t)group * a.N : nullptr;
-  product_rows(sums, smem, [&](int m, int nn, float (&v)[4]) __attribute__((always_inline)) {
-    const int n = n0 + nn;
-    const int cols = a.N - n;
-    if (m >= valid || cols <= 0) return;
-    const int64_t r = m0 + m;
-    if constexpr (!BF16) {
-      const float* const b = reinterpret_cast<const float*>(Bg);
-      redo_not_finite(v, cols < 4 ? cols : 4, reinterpret_cast<const float*>(Ap) + m * a.lda, 1,
-                      C::B_COL ? b + n : b + n * a.ldb, C::B_COL ? a.ldb : 1,
-                      C::B_COL ? 1 : a.ldb, a.K);
-    }
-    if (bias) {
-      float w[4];
-      read4<false>(bias, n, cols, w);
+  const unsigned char* const res =
+      a.residual && !orphans ? static_cast<const unsigned char*>(a.residual) : nullptr;
+  struct Row {
+    float v[V];
+  };
+  product_rows_cols<V>(
+      sums, smem,
+      [&](int m, int nn) __attribute__((always_inline)) {
+        Row x = {};
+        if (res && m < valid && n0 + nn < a.N)
+          read_row<BF16>(res + (m0 + m) * a.ldr * C::ESZ, n0 + nn, a.N - n0 - nn, x.v);
+        return x;
+      },
+      [&](int m, int nn, float (&v)[V], const Row& x) __attribute__((always_inline)) {
+        const int n = n0 + nn;
+        const int cols = a.N - n;
+        if (m >= valid || cols <= 0) return;
+        const int64_t r = m0 + m;
+        if constexpr (!BF16) {
+          const float* const b = reinterpret_cast<const float*>(Bg);
+          redo_not_finite(v, cols < 4 ? cols : 4, reinterpret_cast<const float*>(Ap) + m * a.lda, 1,
+                          C::B_COL ? b + n : b + n * a.ldb, C::B_COL ? a.ldb : 1,
+                          C::B_COL ? 1 : a.ldb, a.K);
+        }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] += w[e];
-    }
-    if (a.U) write4<BF16>(static_cast<unsigned char*>(a.U) + r * a.ldu * C::ESZ, n, cols, v);
+        for (int e = 0; e < V; ++e) v[e] += bias[e];
+        if (a.U)
+          write_row<BF16>(static_cast<unsigned char*>(a.U) + r * a.ldu * C::ESZ, n, cols, v);
+        if (a.act != kActNone)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = activate(v[e], a.act);
-    if (a.residual && !orphans) {
-      float w[4];
-      read4<BF16>(static_cast<const unsigned char*>(a.residual) + r * a.ldr * C::ESZ, n, cols, w);
+          for (int e = 0; e < V; ++e) v[e] = activate(v[e], a.act);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] += w[e];
-    }
-    write4<BF16>(static_cast<unsigned char*>(a.C) + r * a.ldc * C::ESZ, n, cols, v);
-  });
+        for (int e = 0; e < V; ++e) v[e] += x.v[e];
+        write_row<BF16>(static_cast<unsigned char*>(a.C) + r * a.ldc * C::ESZ, n, cols, v);
+      },
+      [](int, int, const float (&)[8]) {}, false);
+}
+
+template <class C>
+__global__ __launch_bounds__(C::THREADS, C::WPE) void dense_rows_kernel(DenseLaunch a) {
+  __shared__ __attribute__((aligned(16))) unsigned char smem[C::LDS_BYTES];
+  rows_block<C>(a, blockIdx.x, gridDim.x, smem);
 }
 
 // ---- the forward pass of few rows ---------------------------------------------
@@ -283,20 +328,20 @@ __device__ __forceinline__ void few_rows(const DenseLaunch& a, const unsigned ch
       const int64_t r = r0 + m;
       if (a.bias && !orphans) {
         float w[4];
-        read4<false>(a.bias + (int64_t)group * a.N, n, cols, w);
+        read_row<false>(a.bias + (int64_t)group * a.N, n, cols, w);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] += w[e];
       }
-      if (a.U) write4<BF16>(static_cast<unsigned char*>(a.U) + r * a.ldu * ESZ, n, cols, v);
+      if (a.U) write_row<BF16>(static_cast<unsigned char*>(a.U) + r * a.ldu * ESZ, n, cols, v);
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = activate(v[e], a.act);
       if (a.residual && !orphans) {
         float w[4];
-        read4<BF16>(static_cast<const unsigned char*>(a.residual) + r * a.ldr * ESZ, n, cols, w);
+        read_row<BF16>(static_cast<const unsigned char*>(a.residual) + r * a.ldr * ESZ, n, cols, w);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] += w[e];
       }
-      write4<BF16>(static_cast<unsigned char*>(a.C) + r * a.ldc * ESZ, n, cols, v);
+      write_row<BF16>(static_cast<unsigned char*>(a.C) + r * a.ldc * ESZ, n, cols, v);
     }
   }
   __syncthreads();
@@ -335,7 +380,8 @@ __global__ __launch_bounds__(256) void dense_dz_kernel(DenseGradLaunch a, int la
   const int tid = threadIdx.x;
   Piece p;
   if (a.offsets) {
-    p = Groups{a.offsets, a.G, a.n, a.bias_rows, true, true}.find(blockIdx.x, tid & 63);
+    int t = blockIdx.x;
+    p = Groups{a.offsets, a.G, a.n, a.bias_rows, true, true}.find(tid & 63, t, 0, 0);
     if (p.group < 0) return;
   } else {
     p.group = 0;
@@ -352,14 +398,14 @@ __global__ __launch_bounds__(256) void dense_dz_kernel(DenseGradLaunch a, int la
 #pragma unroll 4
     for (int64_t r = r0 + tid / lanes; r < r1; r += step) {
       float d[4];
-      read4<BF16>(static_cast<const unsigned char*>(a.dy) + r * a.lddy * ESZ, n, cols, d);
+      read_row<BF16>(static_cast<const unsigned char*>(a.dy) + r * a.lddy * ESZ, n, cols, d);
       if (a.act != kActNone) {
         float u[4];
-        read4<BF16>(static_cast<const unsigned char*>(a.U) + r * a.ldu * ESZ, n, cols, u);
+        read_row<BF16>(static_cast<const unsigned char*>(a.U) + r * a.ldu * ESZ, n, cols, u);
 #pragma unroll
         for (int e = 0; e < 4; ++e) d[e] = grad_through(d[e], u[e], a.act);
       }
-      if (a.dz) write4<BF16>(static_cast<unsigned char*>(a.dz) + r * a.lddz * ESZ, n, cols, d);
+      if (a.dz) write_row<BF16>(static_cast<unsigned char*>(a.dz) + r * a.lddz * ESZ, n, cols, d);
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[e] += d[e];
     }
@@ -375,37 +421,8 @@ __global__ __launch_bounds__(256) void dense_dz_kernel(DenseGradLaunch a, int la
       s[2] += x.z;
       s[3] += x.w;
     }
-    write4<false>(a.db_parts + (int64_t)blockIdx.x * a.N, n, cols, s);
+    write_row<false>(a.db_parts + (int64_t)blockIdx.x * a.N, n, cols, s);
   }
-}
-
-// db[g] = the sum of the group's pieces, in order within each of the four
-// threads that share a column.
-__global__ __launch_bounds__(256) void dense_db_kernel(DenseGradLaunch a) {
-  __shared__ float part[4][64];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int g = blockIdx.y, n = blockIdx.x * 64 + lane;
-  int64_t first = 0, pieces = (a.n + a.bias_rows - 1) / a.bias_rows;
-  if (a.offsets) {
-    const Groups gr{a.offsets, a.G, a.n, a.bias_rows, true, true};
-    int before = 0;
-    for (int q = lane; q < g; q += 64) before += gr.pieces(q);
-    first = wave_sum_i32(before);
-    pieces = gr.pieces(g);
-  }
-  // Offsets that overlap could count more pieces than there are.
-  const int64_t all = dense_bias_pieces(a.n, a.offsets ? a.G : 0, a.bias_rows);
-  if (first + pieces > all) pieces = first < all ? all - first : 0;
-  const int64_t per = (pieces + 3) / 4;
-  const int64_t q1 = per * (w + 1) < pieces ? per * (w + 1) : pieces;
-  float s = 0.0f;
-  if (n < a.N)
-#pragma unroll 8
-    for (int64_t q = per * w; q < q1; ++q) s += a.db_parts[(first + q) * a.N + n];
-  part[w][lane] = s;
-  __syncthreads();
-  if (w == 0 && n < a.N)
-    a.db[(int64_t)g * a.N + n] = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
 }
 
 // ---- dW ------------------------------------------------------------------------
@@ -414,29 +431,25 @@ __global__ __launch_bounds__(256) void dense_db_kernel(DenseGradLaunch a) {
 // group of several leaves fp32 partial sums in the workspace, which
 // dense_dw_join_kernel adds in order.
 template <class C>
-__global__ __launch_bounds__(C::THREADS, C::WPE) void dense_dw_kernel(DenseGradLaunch a) {
-  __shared__ __attribute__((aligned(16))) unsigned char smem[C::LDS_BYTES];
+__device__ __forceinline__ void dw_block(const DenseGradLaunch& a, int block, int blocks,
+                                         unsigned char* smem) {
   constexpr bool BF16 = C::MODE == kBf16;
   const int lane = threadIdx.x & 63;
   const int tiles_k = (a.K + C::BN - 1) / C::BN, tiles = tiles_k * ((a.N + C::BM - 1) / C::BM);
   Piece p;
-  int tile;
+  int tile = 0;
   if (a.offsets) {
-    const Groups gr{a.offsets, a.G, a.n, a.piece, true, false};
-    const int total = gr.total(lane) * tiles;
-    if ((int)blockIdx.x >= total) return;
-    tile = xcd_tile(blockIdx.x, total);
-    p = gr.find(tile / tiles, lane);
+    p = Groups{a.offsets, a.G, a.n, a.piece, true, false}.find(lane, tile, block, tiles);
     if (p.group < 0) return;
   } else {
-    tile = xcd_tile(blockIdx.x, gridDim.x);
+    tile = xcd_tile(block, blocks);
     p.group = 0;
     p.lo = 0;
     p.hi = a.n;
     p.index = tile / tiles;
     p.pieces = (int)((a.n + a.piece - 1) / a.piece);
+    tile %= tiles;
   }
-  tile %= tiles;
   const int n0 = tile / tiles_k * C::BM, k0 = tile % tiles_k * C::BN;
   const int64_t r0 = p.lo + p.index * a.piece;
   const int64_t rows = p.hi - r0 < a.piece ? p.hi - r0 : a.piece;
@@ -452,54 +465,103 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void dense_dw_kernel(DenseGradL
   float* const part = p.pieces > 1 ? a.dw_parts + (p.slot + p.index) * (int64_t)a.N * a.K : nullptr;
   unsigned char* const out =
       static_cast<unsigned char*>(a.dW) + (int64_t)p.group * a.N * a.K * C::ESZ;
-  product_rows(sums, smem, [&](int m, int nn, float (&v)[4]) __attribute__((always_inline)) {
-    const int cols = vk - nn;
-    if (m >= vn || cols <= 0) return;
-    if constexpr (!BF16)
-      redo_not_finite(v, cols < 4 ? cols : 4, reinterpret_cast<const float*>(Z) + m, a.lddz,
-                      reinterpret_cast<const float*>(X) + nn, a.ldx, 1, rows);
-    const int64_t at = (int64_t)(n0 + m) * a.K + k0 + nn;
-    if (part) write4<false>(part, at, cols, v);
-    else write4<BF16>(out, at, cols, v);
-  });
+  constexpr int V = BF16 ? 8 : 4;
+  product_rows_cols<V>(
+      sums, smem, [](int, int) { return Nothing{}; },
+      [&](int m, int nn, float (&v)[V], Nothing) __attribute__((always_inline)) {
+        const int cols = vk - nn;
+        if (m >= vn || cols <= 0) return;
+        if constexpr (!BF16)
+          redo_not_finite(v, cols < 4 ? cols : 4, reinterpret_cast<const float*>(Z) + m, a.lddz,
+                          reinterpret_cast<const float*>(X) + nn, a.ldx, 1, rows);
+        const int64_t at = (int64_t)(n0 + m) * a.K + k0 + nn;
+        if (part) write_row<false>(part, at, cols, v);
+        else write_row<BF16>(out, at, cols, v);
+      },
+      [](int, int, const float (&)[8]) {}, false);
 }
 
+template <class C>
+__global__ __launch_bounds__(C::THREADS, C::WPE) void dense_dw_kernel(DenseGradLaunch a) {
+  __shared__ __attribute__((aligned(16))) unsigned char smem[C::LDS_BYTES];
+  dw_block<C>(a, blockIdx.x, gridDim.x, smem);
+}
+
+// dx and dW in one launch, dW's blocks first: neither fills the chip to its end, and
+// for few rows a launch costs as much as either (about 5 us).
+template <class CX, class CW>
+__global__ __launch_bounds__(CX::THREADS, CX::WPE) void dense_grads_kernel(DenseLaunch x,
+                                                                           DenseGradLaunch w,
+                                                                           int w_blocks) {
+  static_assert(CX::THREADS == CW::THREADS, "one block size");
+  __shared__ __attribute__((aligned(16))) unsigned char
+      smem[CX::LDS_BYTES > CW::LDS_BYTES ? CX::LDS_BYTES : CW::LDS_BYTES];
+  if ((int)blockIdx.x < w_blocks) dw_block<CW>(w, blockIdx.x, w_blocks, smem);
+  else rows_block<CX>(x, blockIdx.x - w_blocks, gridDim.x - w_blocks, smem);
+}
+
+// The partial sums, added in order: of dW (blocks below dw_blocks, 2,048 elements
+// each) and of db (64 columns, eight waves' shares of the pieces, in order within
+// each and then over the eight).
+constexpr int kJoinThreads = 512;
 template <bool BF16>
-__global__ __launch_bounds__(256) void dense_dw_join_kernel(DenseGradLaunch a) {
-  const int64_t size = (int64_t)a.N * a.K;
-  Piece p;
+__global__ __launch_bounds__(kJoinThreads) void dense_join_kernel(DenseGradLaunch a, int dw_blocks) {
+  __shared__ float part[kJoinThreads / 64][64];
+  const int lane = threadIdx.x & 63, g = blockIdx.y;
+  const bool of_dw = (int)blockIdx.x < dw_blocks;
+  const int unit = of_dw ? a.piece : a.bias_rows;
+  // The pieces before this group's, and its own.
+  int64_t first = 0, pieces = (a.n + unit - 1) / unit;
   if (a.offsets) {
-    // The group's first piece: pieces before it, then its own.
-    const Groups gr{a.offsets, a.G, a.n, a.piece, true, false};
-    const int lane = threadIdx.x & 63, g = blockIdx.y;
-    p.pieces = gr.pieces(g);
-    if (p.pieces < 2) return;
+    const Groups gr{a.offsets, a.G, a.n, unit, true, !of_dw};
+    pieces = gr.pieces(g);
+    if (of_dw && pieces < 2) return;
     int before = 0;
     for (int q = lane; q < g; q += 64) {
       const int c = gr.pieces(q);
-      before += c > 1 ? c : 0;
+      before += of_dw && c < 2 ? 0 : c;
     }
-    p.group = g;
-    p.slot = wave_sum_i32(before);
-    const int64_t all = dense_dw_parts(a.n, a.piece, a.G);
-    if (p.slot + p.pieces > all) p.pieces = p.slot < all ? (int)(all - p.slot) : 0;
-  } else {
-    p.group = 0;
-    p.pieces = (int)((a.n + a.piece - 1) / a.piece);
+    first = wave_sum_i32(before);
+  } else if (of_dw && pieces < 2) {
+    return;
   }
-  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-  if (at >= size) return;
-  const int cols = (int)(size - at < 4 ? size - at : 4);
-  const float* src = a.dw_parts + p.slot * size;
-  float s[4] = {0, 0, 0, 0};
-#pragma unroll 4
-  for (int q = 0; q < p.pieces; ++q, src += size) {
-    float v[4];
-    read4<false>(src, at, cols, v);
+  // Offsets that overlap could count more pieces than there are.
+  const int groups = a.offsets ? a.G : 0;
+  const int64_t all = of_dw ? dense_dw_parts(a.n, a.piece, groups)
+                            : dense_bias_pieces(a.n, groups, a.bias_rows);
+  if (first + pieces > all) pieces = first < all ? all - first : 0;
+  if (of_dw) {
+    const int64_t size = (int64_t)a.N * a.K;
+    const int64_t at = ((int64_t)blockIdx.x * kJoinThreads + threadIdx.x) * 4;
+    if (at >= size) return;
+    const int cols = (int)(size - at < 4 ? size - at : 4);
+    const float* src = a.dw_parts + first * size;
+    float s[4] = {0, 0, 0, 0};
+#pragma unroll 8
+    for (int64_t q = 0; q < pieces; ++q, src += size) {
+      float v[4];
+      read_row<false>(src, at, cols, v);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s[e] += v[e];
+      for (int e = 0; e < 4; ++e) s[e] += v[e];
+    }
+    write_row<BF16>(static_cast<unsigned char*>(a.dW) + g * size * (BF16 ? 2 : 4), at, cols, s);
+    return;
   }
-  write4<BF16>(static_cast<unsigned char*>(a.dW) + p.group * size * (BF16 ? 2 : 4), at, cols, s);
+  constexpr int kShares = kJoinThreads / 64;
+  const int w = threadIdx.x >> 6, n = ((int)blockIdx.x - dw_blocks) * 64 + lane;
+  const int64_t per = (pieces + kShares - 1) / kShares;
+  const int64_t q1 = per * (w + 1) < pieces ? per * (w + 1) : pieces;
+  float s = 0.0f;
+  if (n < a.N)
+#pragma unroll 8
+    for (int64_t q = per * w; q < q1; ++q) s += a.db_parts[(first + q) * a.N + n];
+  part[w][lane] = s;
+  __syncthreads();
+  if (w == 0 && n < a.N) {
+#pragma unroll
+    for (int q = 1; q < kShares; ++q) s += part[q][lane];
+    a.db[(int64_t)g * a.N + n] = s;
+  }
 }
 
 // ---- tile shapes -----------------------------------------------------------------
@@ -529,9 +591,11 @@ constexpr int side(Shape s) { return s == kSmall ? 64 : (s == kMid ? 128 : 256);
 
 inline int64_t tiles_of(int64_t m, int64_t n, int b) { return ((m + b - 1) / b) * ((n + b - 1) / b); }
 
-inline Shape rows_shape(int64_t m, int64_t n, bool bf16) {
+inline Shape rows_shape(const DenseLaunch& a, bool bf16) {
+  const int64_t m = a.M, n = a.N;
   if (!bf16) return tiles_of(m, n, 128) < 512 ? kSmall : kMid;
   if (tiles_of(m, n, 64) <= 512) return kSmall;
+  if (a.offsets && m < 4096 * (int64_t)a.G) return kMid;
   return tiles_of(m, n, 256) < 256 ? kMid : kBig;
 }
 
@@ -541,19 +605,52 @@ inline bool vectors(const void* p, int64_t ld, int64_t width, bool bf16) {
 }
 
 template <class C>
-hipError_t rows_cfg(const DenseLaunch& a, hipStream_t s) {
+int64_t rows_blocks(const DenseLaunch& a) {
   const int64_t tiles_n = (a.N + C::BN - 1) / C::BN;
-  const int64_t tiles = ((a.M + C::BM - 1) / C::BM + (a.offsets ? a.G + 1 : 0)) * tiles_n;
-  if (tiles > 0x7FFFFFFFll) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(dense_rows_kernel<C>, dim3((unsigned)tiles), dim3(C::THREADS), 0, s, a);
+  return ((a.M + C::BM - 1) / C::BM + (a.offsets ? a.G + 1 : 0)) * tiles_n;
+}
+template <class C>
+int64_t dw_blocks(const DenseGradLaunch& a) {
+  const int64_t pieces = (a.n + a.piece - 1) / a.piece + (a.offsets ? a.G : 0);
+  return (pieces > 0 ? pieces : 1) * tiles_of(a.N, a.K, C::BM);
+}
+
+template <class C>
+hipError_t rows_cfg(const DenseLaunch& a, hipStream_t s) {
+  const int64_t blocks = rows_blocks<C>(a);
+  if (blocks > 0x7FFFFFFFll) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(dense_rows_kernel<C>, dim3((unsigned)blocks), dim3(C::THREADS), 0, s, a);
   return hipGetLastError();
+}
+template <class C>
+hipError_t dw_cfg(const DenseGradLaunch& a, hipStream_t s) {
+  const int64_t blocks = dw_blocks<C>(a);
+  if (blocks > 0x7FFFFFFFll) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(dense_dw_kernel<C>, dim3((unsigned)blocks), dim3(C::THREADS), 0, s, a);
+  return hipGetLastError();
+}
+template <class CX, class CW>
+hipError_t grads_cfg(const DenseLaunch& x, const DenseGradLaunch& w, hipStream_t s) {
+  const int64_t bw = dw_blocks<CW>(w), bx = rows_blocks<CX>(x);
+  if (bw + bx > 0x7FFFFFFFll) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((dense_grads_kernel<CX, CW>), dim3((unsigned)(bw + bx)), dim3(CX::THREADS), 0, s,
+                     x, w, (int)bw);
+  return hipGetLastError();
+}
+
+template <bool B_COL>
+bool rows_vectors(const DenseLaunch& a) {
+  return vectors(a.A, a.lda, a.K, a.bf16) && vectors(a.B, a.ldb, B_COL ? a.N : a.K, a.bf16);
+}
+bool dw_vectors(const DenseGradLaunch& a) {
+  return vectors(a.dz, a.lddz, a.N, a.bf16) && vectors(a.x, a.ldx, a.K, a.bf16);
 }
 
 template <bool BF16, bool B_COL>
 hipError_t rows_dtype(const DenseLaunch& a, hipStream_t s) {
   using T = Tiles<BF16, false, B_COL>;
-  const Shape shape = rows_shape(a.M, a.N, BF16);
-  if (vectors(a.A, a.lda, a.K, BF16) && vectors(a.B, a.ldb, B_COL ? a.N : a.K, BF16)) {
+  const Shape shape = rows_shape(a, BF16);
+  if (rows_vectors<B_COL>(a)) {
     if (shape == kSmall) return rows_cfg<typename T::RingSmall>(a, s);
     if (shape == kMid) return rows_cfg<typename T::RingMid>(a, s);
     return rows_cfg<typename T::RingBig>(a, s);
@@ -568,20 +665,11 @@ inline Shape dw_shape(int64_t n, int N, int K, bool bf16) {
   return tiles_of(N, K, 128) * (n / 512) >= 256 && N > 64 && K > 64 ? kMid : kSmall;
 }
 
-template <class C>
-hipError_t dw_cfg(const DenseGradLaunch& a, hipStream_t s) {
-  const int64_t pieces = (a.n + a.piece - 1) / a.piece + (a.offsets ? a.G : 0);
-  const int64_t blocks = (pieces > 0 ? pieces : 1) * tiles_of(a.N, a.K, C::BM);
-  if (blocks > 0x7FFFFFFFll) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(dense_dw_kernel<C>, dim3((unsigned)blocks), dim3(C::THREADS), 0, s, a);
-  return hipGetLastError();
-}
-
 template <bool BF16>
-hipError_t dw_tiles(const DenseGradLaunch& a, hipStream_t s) {
+hipError_t dw_dtype(const DenseGradLaunch& a, hipStream_t s) {
   using T = Tiles<BF16, true, true>;
   const Shape shape = dw_shape(a.n, a.N, a.K, BF16);
-  if (vectors(a.dz, a.lddz, a.N, BF16) && vectors(a.x, a.ldx, a.K, BF16)) {
+  if (dw_vectors(a)) {
     if (shape == kSmall) return dw_cfg<typename T::RingSmall>(a, s);
     if (shape == kMid) return dw_cfg<typename T::RingMid>(a, s);
     return dw_cfg<typename T::RingBig>(a, s);
@@ -589,14 +677,18 @@ hipError_t dw_tiles(const DenseGradLaunch& a, hipStream_t s) {
   return shape == kSmall ? dw_cfg<typename T::Small>(a, s) : dw_cfg<typename T::Mid>(a, s);
 }
 
+// Both in one launch where both take ring tiles of four waves.
 template <bool BF16>
-hipError_t dw_dtype(const DenseGradLaunch& a, hipStream_t s) {
-  const hipError_t e = dw_tiles<BF16>(a, s);
-  if (e != hipSuccess || !a.dw_parts) return e;
-  const int64_t blocks = ((int64_t)a.N * a.K + 1023) / 1024;
-  hipLaunchKernelGGL(dense_dw_join_kernel<BF16>, dim3((unsigned)blocks, a.offsets ? a.G : 1),
-                     dim3(256), 0, s, a);
-  return hipGetLastError();
+bool grads_dtype(const DenseLaunch& x, const DenseGradLaunch& w, hipStream_t s, hipError_t* e) {
+  using X = Tiles<BF16, false, true>;
+  using W = Tiles<BF16, true, true>;
+  const Shape sx = rows_shape(x, BF16), sw = dw_shape(w.n, w.N, w.K, BF16);
+  if (sx == kBig || sw == kBig || !rows_vectors<true>(x) || !dw_vectors(w)) return false;
+  if (sx == kSmall && sw == kSmall) *e = grads_cfg<typename X::RingSmall, typename W::RingSmall>(x, w, s);
+  else if (sx == kSmall) *e = grads_cfg<typename X::RingSmall, typename W::RingMid>(x, w, s);
+  else if (sw == kSmall) *e = grads_cfg<typename X::RingMid, typename W::RingSmall>(x, w, s);
+  else *e = grads_cfg<typename X::RingMid, typename W::RingMid>(x, w, s);
+  return true;
 }
 
 bool few_rows_wanted(const DenseLaunch& a) {
@@ -618,36 +710,54 @@ hipError_t launch_dense_rows(const DenseLaunch& a, hipStream_t s) {
   return a.bf16 ? rows_dtype<true, false>(a, s) : rows_dtype<false, false>(a, s);
 }
 
-// Rows per piece of dW's sums: as many pieces as give the chip 512 blocks, of 256
-// rows at least.
+// Rows per piece of dW's sums: pieces that give every CU one round of blocks (one
+// block of 256 x 256, two of the others), of 256 rows at least. Under more pieces
+// the partial sums cost more than the even ends save (60,000 rows in 64 groups,
+// 512 x 1,024: 960 rows 154 us with the sums, 1,920 rows 127).
 int64_t dense_dw_piece(int64_t n, int N, int K, bool bf16) {
-  const int64_t tiles = tiles_of(N, K, side(dw_shape(n, N, K, bf16)));
-  const int64_t want = (512 + tiles - 1) / tiles;
+  const Shape shape = dw_shape(n, N, K, bf16);
+  const int64_t tiles = tiles_of(N, K, side(shape)), blocks = shape == kBig ? 256 : 512;
+  const int64_t want = (blocks + tiles - 1) / tiles;
   const int64_t rows = ((n + want - 1) / want + 63) / 64 * 64;
   return rows < 256 ? 256 : rows;
 }
 
 hipError_t launch_dense_dz(const DenseGradLaunch& a, hipStream_t s) {
+  const int64_t pieces = dense_bias_pieces(a.n, a.offsets ? a.G : 0, a.bias_rows);
+  if (pieces <= 0) return hipSuccess;
   ProfileScope prof(kKDenseGrad, s);
   int lanes = 1;
   while (lanes < 64 && lanes * 4 < a.N) lanes *= 2;
-  const int64_t pieces = dense_bias_pieces(a.n, a.offsets ? a.G : 0, a.bias_rows);
-  const dim3 grid((unsigned)(pieces > 0 ? pieces : 1), (unsigned)((a.N + 4 * lanes - 1) / (4 * lanes)));
-  if (pieces > 0) {
-    if (a.bf16) hipLaunchKernelGGL(dense_dz_kernel<true>, grid, dim3(256), 0, s, a, lanes);
-    else hipLaunchKernelGGL(dense_dz_kernel<false>, grid, dim3(256), 0, s, a, lanes);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  if (!a.db) return hipSuccess;
-  hipLaunchKernelGGL(dense_db_kernel, dim3((unsigned)((a.N + 63) / 64), a.offsets ? a.G : 1),
-                     dim3(256), 0, s, a);
+  const dim3 grid((unsigned)pieces, (unsigned)((a.N + 4 * lanes - 1) / (4 * lanes)));
+  if (a.bf16) hipLaunchKernelGGL(dense_dz_kernel<true>, grid, dim3(256), 0, s, a, lanes);
+  else hipLaunchKernelGGL(dense_dz_kernel<false>, grid, dim3(256), 0, s, a, lanes);
   return hipGetLastError();
 }
 
 hipError_t launch_dense_dw(const DenseGradLaunch& a, hipStream_t s) {
   ProfileScope prof(kKDenseGrad, s);
   return a.bf16 ? dw_dtype<true>(a, s) : dw_dtype<false>(a, s);
+}
+
+hipError_t launch_dense_dx_dw(const DenseLaunch& x, const DenseGradLaunch& w, hipStream_t s) {
+  {
+    ProfileScope prof(kKDenseGrad, s);
+    hipError_t e = hipSuccess;
+    if (w.bf16 ? grads_dtype<true>(x, w, s, &e) : grads_dtype<false>(x, w, s, &e)) return e;
+  }
+  const hipError_t e = launch_dense_rows(x, s);
+  return e != hipSuccess ? e : launch_dense_dw(w, s);
+}
+
+hipError_t launch_dense_join(const DenseGradLaunch& a, hipStream_t s) {
+  const int64_t dw = a.dW && a.dw_parts ? ((int64_t)a.N * a.K + 4 * kJoinThreads - 1) / (4 * kJoinThreads) : 0;
+  const int64_t db = a.db ? (a.N + 63) / 64 : 0;
+  if (dw + db == 0) return hipSuccess;
+  ProfileScope prof(kKDenseGrad, s);
+  const dim3 grid((unsigned)(dw + db), a.offsets ? a.G : 1);
+  if (a.bf16) hipLaunchKernelGGL(dense_join_kernel<true>, grid, dim3(kJoinThreads), 0, s, a, (int)dw);
+  else hipLaunchKernelGGL(dense_join_kernel<false>, grid, dim3(kJoinThreads), 0, s, a, (int)dw);
+  return hipGetLastError();
 }
 
 }  // namespace pinsage

@@ -293,7 +293,7 @@ struct DenseLaunch {
 };
 hipError_t launch_dense_rows(const DenseLaunch& a, hipStream_t s);
 
-// dz = dy * act'(U) and db (launch_dense_dz), dW[g] = dz^T x (launch_dense_dw) over
+// dz = dy * act'(U) and db's partial sums (launch_dense_dz), dW[g] = dz^T x over
 // n rows of N outputs and K inputs. dz may be null (nothing written; dW then reads
 // dy as its dz, which the caller passes in `dz` of the second launch).
 struct DenseGradLaunch {
@@ -335,6 +335,9 @@ __host__ __device__ inline int64_t dense_dw_parts(int64_t n, int64_t piece, int 
 }
 hipError_t launch_dense_dz(const DenseGradLaunch& a, hipStream_t s);
 hipError_t launch_dense_dw(const DenseGradLaunch& a, hipStream_t s);
+hipError_t launch_dense_dx_dw(const DenseLaunch& x, const DenseGradLaunch& w, hipStream_t s);
+// Adds the partial sums of db (after launch_dense_dz) and dW.
+hipError_t launch_dense_join(const DenseGradLaunch& a, hipStream_t s);
 
 // Newton-Schulz orthogonalisation of `batch` matrices [rows][cols] (contiguous), and
 // the optimiser step around it (newton.hip). `update` null: X0 = in / (|in| + eps).

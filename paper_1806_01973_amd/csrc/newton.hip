@@ -57,19 +57,20 @@ __device__ __forceinline__ void put(uint16_t* p, int64_t plane, const float (&v)
   if constexpr (PLANES == 2) *reinterpret_cast<words*>(p + plane) = lo;
 }
 template <int PLANES>
-__device__ __forceinline__ void get4(const uint16_t* p, int64_t plane, float (&v)[4]) {
-  const uint2 hi = *reinterpret_cast<const uint2*>(p);
-  v[0] = unpack_f16(hi.x, 0);
-  v[1] = unpack_f16(hi.x, 1);
-  v[2] = unpack_f16(hi.y, 0);
-  v[3] = unpack_f16(hi.y, 1);
-  if constexpr (PLANES == 2) {
-    const uint2 lo = *reinterpret_cast<const uint2*>(p + plane);
-    v[0] += unpack_f16(lo.x, 0);
-    v[1] += unpack_f16(lo.x, 1);
-    v[2] += unpack_f16(lo.y, 0);
-    v[3] += unpack_f16(lo.y, 1);
-  }
+struct Parts8 {
+  u32x4 p[PLANES];
+};
+template <int PLANES>
+__device__ __forceinline__ Parts8<PLANES> get8(const uint16_t* p, int64_t plane) {
+  Parts8<PLANES> x;
+  x.p[0] = *reinterpret_cast<const u32x4*>(p);
+  if constexpr (PLANES == 2) x.p[1] = *reinterpret_cast<const u32x4*>(p + plane);
+  return x;
+}
+template <int PLANES>
+__device__ __forceinline__ float value(const Parts8<PLANES>& x, int e) {
+  const float hi = unpack_f16(x.p[0][e / 2], e & 1);
+  return PLANES == 2 ? hi + unpack_f16(x.p[PLANES - 1][e / 2], e & 1) : hi;
 }
 
 // ---- the norm, with the momentum's update ---------------------------------------
@@ -77,10 +78,10 @@ __device__ __forceinline__ void get4(const uint16_t* p, int64_t plane, float (&v
 // or the step's combination of it with the already updated momentum.
 template <bool BF16>
 __device__ __forceinline__ void update4(const NewtonLaunch& a, int64_t at, int cols, float (&u)[4]) {
-  read4<BF16>(a.in, at, cols, u);
+  read_row<BF16>(a.in, at, cols, u);
   if (!a.weight) return;
   float m[4];
-  read4<false>(a.momentum_out, at, cols, m);
+  read_row<false>(a.momentum_out, at, cols, m);
 #pragma unroll
   for (int e = 0; e < 4; ++e) u[e] = a.nesterov ? fmaf(a.beta, m[e], u[e]) : m[e];
 }
@@ -96,16 +97,16 @@ __global__ __launch_bounds__(256) void newton_norm_kernel(NewtonLaunch a, Newton
     float u[4];
     if (a.weight) {
       float m[4];
-      read4<BF16>(a.in, base + i, cols, u);
-      read4<false>(a.momentum, base + i, cols, m);
+      read_row<BF16>(a.in, base + i, cols, u);
+      read_row<false>(a.momentum, base + i, cols, m);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         m[e] = fmaf(a.beta, m[e], u[e]);
         u[e] = a.nesterov ? fmaf(a.beta, m[e], u[e]) : m[e];
       }
-      write4<false>(a.momentum_out, base + i, cols, m);
+      write_row<false>(a.momentum_out, base + i, cols, m);
     } else {
-      read4<BF16>(a.in, base + i, cols, u);
+      read_row<BF16>(a.in, base + i, cols, u);
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) s = fma((double)u[e], (double)u[e], s);
@@ -210,24 +211,23 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch
   TileSums<C> sums;
   tile_sums(L, R, 0, depth, smem, sums);
 
-  // Products carry the scale twice.
+  // Products carry the scale twice. What a product is added to is read a band ahead.
   const float back = 1.0f / kScale;
   if constexpr (kSymmetric) {
     uint16_t* const out = KIND == kGram ? A : B;
-    product_rows_cols(
+    product_rows_cols<8>(
         sums, smem,
-        [&](int m, int n, float (&v)[4]) __attribute__((always_inline)) {
-          const int64_t at = (int64_t)(i0 + m) * w.mp + j0 + n;
-          if constexpr (KIND == kGram) {
+        [&](int m, int n) __attribute__((always_inline)) {
+          if constexpr (KIND == kGram) return Nothing{};
+          else return get8<PLANES>(A + (int64_t)(i0 + m) * w.mp + j0 + n, pa);
+        },
+        [&](int m, int n, float (&v)[8], const auto& x) __attribute__((always_inline)) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] *= back;
-          } else {
-            float x[4];
-            get4<PLANES>(A + at, pa, x);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = fmaf(a.b, x[e], a.c * back * v[e]);
+          for (int e = 0; e < 8; ++e) {
+            if constexpr (KIND == kGram) v[e] *= back;
+            else v[e] = fmaf(a.b, value(x, e), a.c * back * v[e]);
           }
-          put<PLANES>(out + at, pa, v);
+          put<PLANES>(out + (int64_t)(i0 + m) * w.mp + j0 + n, pa, v);
         },
         [&](int m, int n, const float (&v)[8]) __attribute__((always_inline)) {
           put<PLANES>(out + (int64_t)(j0 + n) * w.mp + i0 + m, pa, v);
@@ -236,15 +236,15 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch
   } else if constexpr (KIND == kApply) {
     uint16_t* const outx = w.X[1 - from] + z * PLANES * px;
     uint16_t* const outt = w.T[1 - from] + z * PLANES * px;
-    product_rows_cols(
+    product_rows_cols<8>(
         sums, smem,
-        [&](int m, int n, float (&v)[4]) __attribute__((always_inline)) {
-          const int64_t at = (int64_t)(i0 + m) * w.np + j0 + n;
-          float x[4];
-          get4<PLANES>(X + at, px, x);
+        [&](int m, int n) __attribute__((always_inline)) {
+          return get8<PLANES>(X + (int64_t)(i0 + m) * w.np + j0 + n, px);
+        },
+        [&](int m, int n, float (&v)[8], const auto& x) __attribute__((always_inline)) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = fmaf(a.a, x[e], back * v[e]);
-          put<PLANES>(outx + at, px, v);
+          for (int e = 0; e < 8; ++e) v[e] = fmaf(a.a, value(x, e), back * v[e]);
+          put<PLANES>(outx + (int64_t)(i0 + m) * w.np + j0 + n, px, v);
         },
         [&](int m, int n, const float (&v)[8]) __attribute__((always_inline)) {
           put<PLANES>(outt + (int64_t)(j0 + n) * w.mp + i0 + m, px, v);
@@ -252,51 +252,50 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch
         true);
   } else {
     const int64_t base = z * a.rows * a.cols;
-    // Up to four results of one row of G, from `at` on.
-    auto give = [&](int64_t at, int cols, float (&y)[4]) __attribute__((always_inline)) {
+    // Up to eight results of one row of G, from `at` on.
+    auto give = [&](int64_t at, int cols, float (&y)[8]) __attribute__((always_inline)) {
       if (a.weight) {
-        float old[4];
-        read4<BF16>(a.weight, at, cols, old);
+        float old[8];
+        read_row<BF16>(a.weight, at, cols, old);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = fmaf(a.decay, old[e], -a.rate * y[e]);
+        for (int e = 0; e < 8; ++e) y[e] = fmaf(a.decay, old[e], -a.rate * y[e]);
       }
-      write4<BF16>(a.out, at, cols, y);
+      write_row<BF16>(a.out, at, cols, y);
     };
-    product_rows_cols(
+    product_rows_cols<8>(
         sums, smem,
-        [&](int m, int n, float (&v)[4]) __attribute__((always_inline)) {
+        [&](int m, int n) __attribute__((always_inline)) {
+          return get8<PLANES>(X + (int64_t)(i0 + m) * w.np + j0 + n, px);
+        },
+        [&](int m, int n, float (&v)[8], const auto& x) __attribute__((always_inline)) {
           const int i = i0 + m, j = j0 + n;
-          float x[4];
-          get4<PLANES>(X + (int64_t)i * w.np + j, px, x);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = fmaf(a.a, x[e], back * v[e]) * back;
+          for (int e = 0; e < 8; ++e) v[e] = fmaf(a.a, value(x, e), back * v[e]) * back;
           if (!w.flip && i < w.m && j < w.n) give(base + (int64_t)i * a.cols + j, w.n - j, v);
         },
         [&](int m, int n, const float (&v)[8]) __attribute__((always_inline)) {
           const int i = i0 + m, j = j0 + n;
-          if (j >= w.n) return;
+          float y[8];
 #pragma unroll
-          for (int h = 0; h < 8; h += 4) {
-            float y[4] = {v[h], v[h + 1], v[h + 2], v[h + 3]};
-            if (i + h < w.m) give(base + (int64_t)j * a.cols + i + h, w.m - i - h, y);
-          }
+          for (int e = 0; e < 8; ++e) y[e] = v[e];
+          if (i < w.m && j < w.n) give(base + (int64_t)j * a.cols + i, w.m - i, y);
         },
         w.flip);
   }
 }
 
 // ---- tile shapes --------------------------------------------------------------------
-// Small tiles as long as all run at once, two blocks per CU: fp16, K = 2,048, 512 tiles
-// of 64 x 64 17.0 us against 19.9 for 128 of 128 x 128 and 1,024 37.0 against 24.1;
-// two parts 59.5 against 57.0 us at 1,024 tiles of 64 x 64. Of the fp16 128 x 128 tiles
-// the ring of four stages while there is one tile per CU (24.9 against 26.1 us), else
-// two blocks of two stages.
+// Measured at depth 2,048, us (fp16): 64 x 64 tiles with four stages, two blocks per
+// CU, 10.8 at 256 tiles and 23.8 at 529; with two stages, which more of them share a
+// CU, 18.4, 20.8 and 27.8 at 1,024; 128 x 128 with four stages 23.9 at 256 tiles (as
+// 1,024 of 64 x 64), with two 28.2, but 75 against 103 at 1,876 tiles of depth 1,024.
+// Two parts: 64 x 64 59.6 at 1,024 tiles, 128 x 128 57.0.
 inline int64_t tiles_of(const NewtonWork& w, int64_t batch, bool symmetric, int side) {
   const int64_t tm = (w.mp + side - 1) / side, tn = (w.np + side - 1) / side;
   return (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batch;
 }
 inline bool small_tiles(const NewtonWork& w, int64_t batch, bool symmetric, bool bf16) {
-  return tiles_of(w, batch, symmetric, 64) <= (bf16 ? 576 : 1024);
+  return tiles_of(w, batch, symmetric, 64) <= (bf16 ? 768 : 1024);
 }
 
 template <class C, int KIND, bool BF16>
@@ -311,8 +310,10 @@ void launch_product(const NewtonLaunch& a, const NewtonWork& w, int from, hipStr
   constexpr bool kSymmetric = KIND == kGram || KIND == kSquare;
   const bool small = small_tiles(w, a.batch, kSymmetric, BF16);
   if constexpr (BF16) {
-    if (small)
+    if (small && tiles_of(w, a.batch, kSymmetric, 64) <= 512)
       launch_one<RingCfg<kF16, 64, 64, 64, 2, 2, false, false, 4>, KIND, true>(a, w, from, s);
+    else if (small)
+      launch_one<RingCfg<kF16, 64, 64, 64, 2, 2, false, false, 2>, KIND, true>(a, w, from, s);
     else if (tiles_of(w, a.batch, kSymmetric, 128) <= 256)
       launch_one<RingCfg<kF16, 128, 128, 64, 2, 2, false, false, 4>, KIND, true>(a, w, from, s);
     else

@@ -88,55 +88,65 @@ __device__ __forceinline__ void store_any(void* p, const T& v) {
   __builtin_memcpy(p, &v, sizeof(T));
 }
 
-// Four elements of a row from column n on, `cols` of which exist; any alignment.
-template <bool BF16>
-__device__ __forceinline__ void read4(const void* row, int64_t n, int cols, float (&v)[4]) {
+// N (4 or 8) elements of a row from column n on, `cols` of which exist; any alignment.
+template <bool BF16, int N>
+__device__ __forceinline__ void read_row(const void* row, int64_t n, int cols, float (&v)[N]) {
   if constexpr (BF16) {
     const uint16_t* const p = static_cast<const uint16_t*>(row) + n;
-    if (cols >= 4) {
-      const uint2 w = load_any<uint2>(p);
-      v[0] = __uint_as_float(w.x << 16);
-      v[1] = __uint_as_float(w.x & 0xFFFF0000u);
-      v[2] = __uint_as_float(w.y << 16);
-      v[3] = __uint_as_float(w.y & 0xFFFF0000u);
+    if (cols >= N) {
+      typedef uint32_t words __attribute__((ext_vector_type(N / 2)));
+      const words w = load_any<words>(p);
+#pragma unroll
+      for (int e = 0; e < N / 2; ++e) {
+        v[2 * e] = __uint_as_float(w[e] << 16);
+        v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+      }
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = e < cols ? bf16_to_f32(p[e]) : 0.0f;
+      for (int e = 0; e < N; ++e) v[e] = e < cols ? bf16_to_f32(p[e]) : 0.0f;
     }
   } else {
     const float* const p = static_cast<const float*>(row) + n;
-    if (cols >= 4) {
-      const float4 w = load_any<float4>(p);
-      v[0] = w.x;
-      v[1] = w.y;
-      v[2] = w.z;
-      v[3] = w.w;
+    if (cols >= N) {
+#pragma unroll
+      for (int q = 0; q < N / 4; ++q) {
+        const float4 w = load_any<float4>(p + 4 * q);
+        v[4 * q] = w.x;
+        v[4 * q + 1] = w.y;
+        v[4 * q + 2] = w.z;
+        v[4 * q + 3] = w.w;
+      }
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = e < cols ? p[e] : 0.0f;
+      for (int e = 0; e < N; ++e) v[e] = e < cols ? p[e] : 0.0f;
     }
   }
 }
 
-template <bool BF16>
-__device__ __forceinline__ void write4(void* row, int64_t n, int cols, const float (&v)[4]) {
+template <bool BF16, int N>
+__device__ __forceinline__ void write_row(void* row, int64_t n, int cols, const float (&v)[N]) {
   if constexpr (BF16) {
     uint16_t* const p = static_cast<uint16_t*>(row) + n;
-    const uint2 w = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-    if (cols >= 4) {
+    typedef uint32_t words __attribute__((ext_vector_type(N / 2)));
+    words w;
+#pragma unroll
+    for (int e = 0; e < N / 2; ++e) w[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+    if (cols >= N) {
       store_any(p, w);
     } else {
-      if (cols > 0) p[0] = (uint16_t)w.x;
-      if (cols > 1) p[1] = (uint16_t)(w.x >> 16);
-      if (cols > 2) p[2] = (uint16_t)w.y;
+#pragma unroll
+      for (int e = 0; e < N - 1; ++e)
+        if (e < cols) p[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
     }
   } else {
     float* const p = static_cast<float*>(row) + n;
-    if (cols >= 4) {
-      store_any(p, make_float4(v[0], v[1], v[2], v[3]));
+    if (cols >= N) {
+#pragma unroll
+      for (int q = 0; q < N / 4; ++q)
+        store_any(p + 4 * q, make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]));
     } else {
 #pragma unroll
-      for (int e = 0; e < 3; ++e)
+      for (int e = 0; e < N - 1; ++e)
         if (e < cols) p[e] = v[e];
     }
   }
@@ -394,19 +404,34 @@ __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B,
   }
 }
 
-// Hands the tile out in whole rows: f(m, n, v) with the tile's row m and its
-// columns n .. n + 3, a wave's lanes side by side along the columns, then, when
-// `turned`, by columns: g(m, n, v) with rows m .. m + 7 of column n, of the values
-// that f left in v. A wave's bands of 32 rows pass through LDS of its own.
-template <class C, class F, class G>
-__device__ __forceinline__ void product_rows_cols(const TileSums<C>& sums, unsigned char* smem, F f,
-                                                  G g, bool turned) {
+// The column within the tile from which this lane gets its V values of every row.
+template <class C, int V>
+__device__ __forceinline__ int product_column() {
+  const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63;
+  return wave % C::WAVES_N * C::WN + lane % (C::WN / V) * V;
+}
+
+// Hands the tile out in whole rows, V columns a lane, a wave's lanes side by side
+// along them: f(m, n, v, x) with the tile's row m, columns n .. n + V - 1 and
+// x = fetch(m, n), called for a band of 32 rows ahead of it (what the epilogue
+// reads is then in flight together); then, when `turned`, by columns: g(m, n, v)
+// with rows m .. m + 7 of column n, of the values that f left in v. A wave's bands
+// pass through LDS of its own.
+template <int V, class C, class P, class F, class G>
+__device__ __forceinline__ void product_rows_cols(const TileSums<C>& sums, unsigned char* smem,
+                                                  P fetch, F f, G g, bool turned) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   float* const stage = reinterpret_cast<float*>(smem + wave * C::STAGE_BYTES);
-  constexpr int WIDTH = C::WN, LANES = WIDTH / 4;  // per row
+  constexpr int WIDTH = C::WN, LANES = WIDTH / V;      // lanes per row
+  constexpr int ROWS = 64 / LANES, PASSES = 32 / ROWS;  // rows at once
+  const int r_lane = lane / LANES, col = lane % LANES * V;
 #pragma unroll
   for (int i = 0; i < C::TM; ++i) {
+    const int m0 = sums.row0 + 32 * i;
+    decltype(fetch(0, 0)) ahead[PASSES];
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) ahead[p] = fetch(m0 + ROWS * p + r_lane, sums.col0 + col);
 #pragma unroll
     for (int j = 0; j < C::TN; ++j)
 #pragma unroll
@@ -416,25 +441,32 @@ __device__ __forceinline__ void product_rows_cols(const TileSums<C>& sums, unsig
             make_float4(sums.v[i][j][4 * q], sums.v[i][j][4 * q + 1], sums.v[i][j][4 * q + 2],
                         sums.v[i][j][4 * q + 3]);
     wave_lds_sync();
-    const int m0 = sums.row0 + 32 * i;
 #pragma unroll
-    for (int r0 = 0; r0 < 32; r0 += 64 / LANES) {
-      const int r = r0 + lane / LANES, col = lane % LANES * 4;
-      float4* const at = reinterpret_cast<float4*>(stage + r * C::STAGE_LD + col);
-      const float4 x = *at;
-      float v[4] = {x.x, x.y, x.z, x.w};
-      f(m0 + r, sums.col0 + col, v);
-      if (turned) *at = make_float4(v[0], v[1], v[2], v[3]);
+    for (int p = 0; p < PASSES; ++p) {
+      float* const at = stage + (ROWS * p + r_lane) * C::STAGE_LD + col;
+      float v[V];
+#pragma unroll
+      for (int q = 0; q < V; q += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(at + q);
+        v[q] = x.x;
+        v[q + 1] = x.y;
+        v[q + 2] = x.z;
+        v[q + 3] = x.w;
+      }
+      f(m0 + ROWS * p + r_lane, sums.col0 + col, v, ahead[p]);
+      if (turned)
+#pragma unroll
+        for (int q = 0; q < V; q += 4)
+          *reinterpret_cast<float4*>(at + q) = make_float4(v[q], v[q + 1], v[q + 2], v[q + 3]);
     }
     wave_lds_sync();
     if (turned) {
-      constexpr int PER = 64 / WIDTH > 0 ? 64 / WIDTH : 1;  // groups of eight rows at once
+      constexpr int COLS = WIDTH < 64 ? WIDTH : 64;  // columns at once, 64 / COLS row groups
 #pragma unroll
       for (int c0 = 0; c0 < WIDTH; c0 += 64)
 #pragma unroll
-        for (int r0 = 0; r0 < 32; r0 += 8 * PER) {
-          const int n = c0 + lane % (WIDTH < 64 ? WIDTH : 64);
-          const int r = r0 + 8 * (lane / (WIDTH < 64 ? WIDTH : 64));
+        for (int r0 = 0; r0 < 32; r0 += 8 * (64 / COLS)) {
+          const int n = c0 + lane % COLS, r = r0 + 8 * (lane / COLS);
           float v[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] = stage[(r + e) * C::STAGE_LD + n];
@@ -445,14 +477,11 @@ __device__ __forceinline__ void product_rows_cols(const TileSums<C>& sums, unsig
   }
 }
 
-template <class C, class F>
-__device__ __forceinline__ void product_rows(const TileSums<C>& sums, unsigned char* smem, F f) {
-  product_rows_cols(sums, smem, f, [](int, int, const float (&)[8]) {}, false);
-}
+struct Nothing {};
 
-// Elements of a row's four that a split product left without a finite value,
-// again as fp32 dot products over `count` columns of k (a: the row, b: the first
-// of the four columns, b_next apart).
+// Of four elements of a row, `cols` of which exist, those that a split product left
+// without a finite value, again as fp32 dot products over `count` columns of k (a:
+// the row, b: the first of the four columns, b_next apart).
 __device__ __forceinline__ void redo_not_finite(float (&v)[4], int cols, const float* a,
                                                 int64_t a_step, const float* b, int64_t b_step,
                                                 int64_t b_next, int64_t count) {
