@@ -1749,9 +1749,9 @@ struct DenseWs {
 DenseWs dense_ws(const pinsage_dense_t* d, int64_t n) {
   DenseWs w;
   w.lddz = (d->d_out + 7) / 8 * 8;
-  w.piece = dense_dw_piece(n, d->d_out, d->d_in, d->dtype == PINSAGE_BF16);
+  w.piece = dense_dw_piece(n, d->d_out, d->d_in, d->num_groups, d->dtype == PINSAGE_BF16);
   if (d->activation != PINSAGE_ACT_NONE) w.dz = align_up((size_t)n * w.lddz * elem_size(d->dtype));
-  w.db = align_up((size_t)dense_bias_pieces(n, d->num_groups, dense_bias_rows(n, d->d_out)) * d->d_out * 4);
+  w.db = align_up((size_t)dense_bias_pieces(n, d->num_groups, dense_bias_rows(n, d->d_out, d->dtype == PINSAGE_BF16)) * d->d_out * 4);
   w.dw = align_up((size_t)dense_dw_parts(n, w.piece, d->num_groups) * d->d_out * d->d_in * 4);
   return w;
 }
@@ -1884,7 +1884,7 @@ int pinsage_dense_backward(const pinsage_dense_t* layer, const void* dy, int64_t
   g.lddz = w.lddz;
   g.db = db;
   g.db_parts = db ? reinterpret_cast<float*>(ws + w.dz) : nullptr;
-  g.bias_rows = dense_bias_rows(n, layer->d_out);
+  g.bias_rows = dense_bias_rows(n, layer->d_out, layer->dtype == PINSAGE_BF16);
   g.dW = dW;
   g.dw_parts = w.dw ? reinterpret_cast<float*>(ws + w.dz + w.db) : nullptr;
   g.piece = (int)w.piece;

@@ -25,26 +25,46 @@ namespace {
 constexpr float kGelu2 = 1.5957691216057308f;  // 2 sqrt(2 / pi)
 constexpr float kGeluCube = 0.044715f;
 
-__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + __expf(-x)); }
-
-__device__ __forceinline__ float activate(float u, int act) {
-  if (act == kActRelu) return u < 0.0f ? 0.0f : u;  // NaN stays
-  if (act == kActGelu) return u * sigmoid(kGelu2 * (u + kGeluCube * u * u * u));
-  if (act == kActSilu) return u * sigmoid(u);
-  return u;
+// The reciprocal instruction is within 1 unit in the last place.
+__device__ __forceinline__ float sigmoid(float x) {
+  return __builtin_amdgcn_rcpf(1.0f + __expf(-x));
 }
 
-__device__ __forceinline__ float grad_through(float dy, float u, int act) {
-  if (act == kActRelu) return u > 0.0f ? dy : 0.0f;
-  if (act == kActGelu) {
-    const float s = sigmoid(kGelu2 * (u + kGeluCube * u * u * u));
-    return dy * (s + u * s * (1.0f - s) * kGelu2 * (1.0f + 3.0f * kGeluCube * u * u));
+// One branch for all values, not one for each.
+template <int N>
+__device__ __forceinline__ void activate(float (&u)[N], int act) {
+  if (act == kActRelu) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) u[e] = u[e] < 0.0f ? 0.0f : u[e];  // NaN stays
+  } else if (act == kActGelu) {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      u[e] *= sigmoid(kGelu2 * (u[e] + kGeluCube * u[e] * u[e] * u[e]));
+  } else if (act == kActSilu) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) u[e] *= sigmoid(u[e]);
   }
-  if (act == kActSilu) {
-    const float s = sigmoid(u);
-    return dy * (s * (1.0f + u * (1.0f - s)));
+}
+
+// dy becomes dy * act'(u).
+template <int N>
+__device__ __forceinline__ void grad_through(float (&dy)[N], const float (&u)[N], int act) {
+  if (act == kActRelu) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) dy[e] = u[e] > 0.0f ? dy[e] : 0.0f;
+  } else if (act == kActGelu) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float q = kGeluCube * u[e] * u[e], s = sigmoid(kGelu2 * u[e] * (1.0f + q));
+      dy[e] *= s + u[e] * s * (1.0f - s) * kGelu2 * (1.0f + 3.0f * q);
+    }
+  } else if (act == kActSilu) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float s = sigmoid(u[e]);
+      dy[e] *= s * (1.0f + u[e] * (1.0f - s));
+    }
   }
-  return dy;
 }
 
 // ---- groups of rows ----------------------------------------------------------
@@ -216,9 +236,7 @@ __device__ __forceinline__ void rows_block(const DenseLaunch& a, int block, int 
         for (int e = 0; e < V; ++e) v[e] += bias[e];
         if (a.U)
           write_row<BF16>(static_cast<unsigned char*>(a.U) + r * a.ldu * C::ESZ, n, cols, v);
-        if (a.act != kActNone)
-#pragma unroll
-          for (int e = 0; e < V; ++e) v[e] = activate(v[e], a.act);
+        activate(v, a.act);
 #pragma unroll
         for (int e = 0; e < V; ++e) v[e] += x.v[e];
         write_row<BF16>(static_cast<unsigned char*>(a.C) + r * a.ldc * C::ESZ, n, cols, v);
@@ -333,8 +351,7 @@ __device__ __forceinline__ void few_rows(const DenseLaunch& a, const unsigned ch
         for (int e = 0; e < 4; ++e) v[e] += w[e];
       }
       if (a.U) write_row<BF16>(static_cast<unsigned char*>(a.U) + r * a.ldu * ESZ, n, cols, v);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = activate(v[e], a.act);
+      activate(v, a.act);
       if (a.residual && !orphans) {
         float w[4];
         read_row<BF16>(static_cast<const unsigned char*>(a.residual) + r * a.ldr * ESZ, n, cols, w);
@@ -370,13 +387,14 @@ __global__ __launch_bounds__(64 * kFewWaves) void dense_few_kernel(DenseLaunch a
 }
 
 // ---- dz and db -----------------------------------------------------------------
-// A block takes a piece of a.bias_rows rows of one group and up to 256 columns, a
-// thread 4 columns of every (256 / lanes)-th row, lanes the smallest power of two
-// of threads that covers the columns.
+// A block takes a piece of a.bias_rows rows of one group; `lanes` threads (the
+// smallest power of two that covers the columns, 64 at most) lie side by side along a
+// row, 16 bytes each, over (256 / lanes) rows at once, four such in flight. Bound by
+// memory: it reads dy and u and writes dz once.
 template <bool BF16>
 __global__ __launch_bounds__(256) void dense_dz_kernel(DenseGradLaunch a, int lanes) {
-  __shared__ float4 sums[256];
-  constexpr int ESZ = BF16 ? 2 : 4;
+  constexpr int ESZ = BF16 ? 2 : 4, V = 16 / ESZ, DEEP = 4;
+  __shared__ float sums[256][V];
   const int tid = threadIdx.x;
   Piece p;
   if (a.offsets) {
@@ -390,37 +408,45 @@ __global__ __launch_bounds__(256) void dense_dz_kernel(DenseGradLaunch a, int la
     p.index = blockIdx.x;
   }
   const int64_t r0 = p.lo + p.index * a.bias_rows;
-  const int64_t r1 = p.hi - r0 < a.bias_rows ? p.hi : r0 + a.bias_rows;
-  const int n = (blockIdx.y * lanes + tid % lanes) * 4, cols = a.N - n;
-  float s[4] = {0, 0, 0, 0};
-  if (cols > 0) {
+  const int rows = (int)(p.hi - r0 < a.bias_rows ? p.hi - r0 : a.bias_rows);
+  const int n = (blockIdx.y * lanes + tid % lanes) * V, cols = a.N - n;
+  const unsigned char* const dy = static_cast<const unsigned char*>(a.dy) + r0 * a.lddy * ESZ;
+  const unsigned char* const u =
+      a.act != kActNone ? static_cast<const unsigned char*>(a.U) + r0 * a.ldu * ESZ : nullptr;
+  unsigned char* const dz = static_cast<unsigned char*>(a.dz) + r0 * a.lddz * ESZ;
+  float s[V] = {};
+  // `have` is a constant where all V columns exist: no branch between the loads.
+  auto walk = [&](int have) __attribute__((always_inline)) {
     const int step = 256 / lanes;
-#pragma unroll 4
-    for (int64_t r = r0 + tid / lanes; r < r1; r += step) {
-      float d[4];
-      read_row<BF16>(static_cast<const unsigned char*>(a.dy) + r * a.lddy * ESZ, n, cols, d);
-      if (a.act != kActNone) {
-        float u[4];
-        read_row<BF16>(static_cast<const unsigned char*>(a.U) + r * a.ldu * ESZ, n, cols, u);
+    for (int r = tid / lanes; r < rows; r += DEEP * step) {
+      float d[DEEP][V], x[DEEP][V];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) d[e] = grad_through(d[e], u[e], a.act);
+      for (int k = 0; k < DEEP; ++k) {
+        const int64_t q = r + k * step < rows ? r + k * step : r;
+        read_row<BF16>(dy + q * a.lddy * ESZ, n, have, d[k]);
+        if (u) read_row<BF16>(u + q * a.ldu * ESZ, n, have, x[k]);
       }
-      if (a.dz) write_row<BF16>(static_cast<unsigned char*>(a.dz) + r * a.lddz * ESZ, n, cols, d);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] += d[e];
+      for (int k = 0; k < DEEP; ++k) {
+        const int64_t q = r + k * step;
+        if (q >= rows) break;
+        if (u) grad_through(d[k], x[k], a.act);
+        if (a.dz) write_row<BF16>(dz + q * a.lddz * ESZ, n, have, d[k]);
+#pragma unroll
+        for (int e = 0; e < V; ++e) s[e] += d[k][e];
+      }
     }
-  }
+  };
+  if (cols >= V) walk(V);
+  else if (cols > 0) walk(cols);
   if (!a.db_parts) return;
-  sums[tid] = make_float4(s[0], s[1], s[2], s[3]);
+#pragma unroll
+  for (int e = 0; e < V; ++e) sums[tid][e] = s[e];
   __syncthreads();
   if (tid < lanes && cols > 0) {
-    for (int t = tid + lanes; t < 256; t += lanes) {
-      const float4 x = sums[t];
-      s[0] += x.x;
-      s[1] += x.y;
-      s[2] += x.z;
-      s[3] += x.w;
-    }
+    for (int t = tid + lanes; t < 256; t += lanes)
+#pragma unroll
+      for (int e = 0; e < V; ++e) s[e] += sums[t][e];
     write_row<false>(a.db_parts + (int64_t)blockIdx.x * a.N, n, cols, s);
   }
 }
@@ -500,67 +526,101 @@ __global__ __launch_bounds__(CX::THREADS, CX::WPE) void dense_grads_kernel(Dense
   else rows_block<CX>(x, blockIdx.x - w_blocks, gridDim.x - w_blocks, smem);
 }
 
-// The partial sums, added in order: of dW (blocks below dw_blocks, 2,048 elements
-// each) and of db (64 columns, eight waves' shares of the pieces, in order within
-// each and then over the eight).
-constexpr int kJoinThreads = 512;
+// The partial sums, added in order: of dW (blocks below dw_blocks) and of db. An item
+// is 256 elements of a group that has partial sums; `shares` (1, 4 or 16) of a
+// block's 16 waves add its pieces, in order within each and then over the shares.
+constexpr int kJoinWaves = 16;
 template <bool BF16>
-__global__ __launch_bounds__(kJoinThreads) void dense_join_kernel(DenseGradLaunch a, int dw_blocks) {
-  __shared__ float part[kJoinThreads / 64][64];
-  const int lane = threadIdx.x & 63, g = blockIdx.y;
+__global__ __launch_bounds__(64 * kJoinWaves) void dense_join_kernel(DenseGradLaunch a,
+                                                                     int dw_blocks, int dw_shares,
+                                                                     int db_shares) {
+  __shared__ float4 part[kJoinWaves][64];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const bool of_dw = (int)blockIdx.x < dw_blocks;
-  const int unit = of_dw ? a.piece : a.bias_rows;
-  // The pieces before this group's, and its own.
-  int64_t first = 0, pieces = (a.n + unit - 1) / unit;
-  if (a.offsets) {
-    const Groups gr{a.offsets, a.G, a.n, unit, true, !of_dw};
-    pieces = gr.pieces(g);
-    if (of_dw && pieces < 2) return;
-    int before = 0;
-    for (int q = lane; q < g; q += 64) {
-      const int c = gr.pieces(q);
-      before += of_dw && c < 2 ? 0 : c;
-    }
-    first = wave_sum_i32(before);
-  } else if (of_dw && pieces < 2) {
-    return;
+  const int shares = of_dw ? dw_shares : db_shares, per_block = kJoinWaves / shares;
+  const int unit = of_dw ? a.piece : a.bias_rows, groups = a.offsets ? a.G : 0;
+  const int64_t size = of_dw ? (int64_t)a.N * a.K : a.N;
+  const uint32_t chunks = (uint32_t)((size + 255) / 256);
+  const Groups gr{a.offsets, a.G, a.n, unit, true, !of_dw};
+  uint32_t items = chunks;
+  if (groups) {
+    uint32_t several = of_dw ? 0 : groups;
+    if (of_dw)
+      for (int g0 = 0; g0 < groups; g0 += 64)
+        several += __popcll(__ballot(g0 + lane < groups && gr.pieces(g0 + lane) > 1));
+    items *= several;
   }
+  const uint32_t blocks = of_dw ? dw_blocks : gridDim.x - dw_blocks;
   // Offsets that overlap could count more pieces than there are.
-  const int groups = a.offsets ? a.G : 0;
   const int64_t all = of_dw ? dense_dw_parts(a.n, a.piece, groups)
                             : dense_bias_pieces(a.n, groups, a.bias_rows);
-  if (first + pieces > all) pieces = first < all ? all - first : 0;
-  if (of_dw) {
-    const int64_t size = (int64_t)a.N * a.K;
-    const int64_t at = ((int64_t)blockIdx.x * kJoinThreads + threadIdx.x) * 4;
-    if (at >= size) return;
-    const int cols = (int)(size - at < 4 ? size - at : 4);
-    const float* src = a.dw_parts + first * size;
+  const float* const parts = of_dw ? a.dw_parts : a.db_parts;
+  for (uint32_t item0 = (of_dw ? blockIdx.x : blockIdx.x - dw_blocks) * per_block; item0 < items;
+       item0 += blocks * per_block) {
+    const uint32_t item = item0 + w / shares;
+    const int share = w % shares;
+    int g = (int)(item / chunks), cols = 0;
+    const int64_t at = (int64_t)(item % chunks) * 256 + lane * 4;
     float s[4] = {0, 0, 0, 0};
-#pragma unroll 8
-    for (int64_t q = 0; q < pieces; ++q, src += size) {
-      float v[4];
-      read_row<false>(src, at, cols, v);
+    if (item < items) {
+      int64_t first = 0, pieces = (a.n + unit - 1) / unit;
+      if (groups) {
+        // The g-th group that counts, its pieces and those before it.
+        int seen = 0, before = 0;
+        for (int g0 = 0; g0 < groups; g0 += 64) {
+          const int p = g0 + lane < groups ? gr.pieces(g0 + lane) : 0;
+          const bool counts = p > (of_dw ? 1 : 0);
+          const int rank = seen + wave_inclusive_sum(counts, lane);
+          const int end = before + wave_inclusive_sum(counts ? p : 0, lane);
+          const unsigned long long hit = __ballot(counts && rank == g + 1);
+          if (hit) {
+            const int l = __builtin_ctzll(hit);
+            pieces = __builtin_amdgcn_readlane(p, l);
+            first = __builtin_amdgcn_readlane(end, l) - pieces;
+            g = g0 + l;
+            break;
+          }
+          seen = __builtin_amdgcn_readlane(rank, 63);
+          before = __builtin_amdgcn_readlane(end, 63);
+        }
+      }
+      if (first + pieces > all) pieces = first < all ? all - first : 0;
+      const int per = (int)((pieces + shares - 1) / shares);
+      const int64_t q0 = (int64_t)per * share;
+      const int count = (int)(q0 >= pieces ? 0 : (pieces - q0 < per ? pieces - q0 : per));
+      cols = (int)(size - at < 4 ? size - at : 4);
+      const float* src = parts + (first + q0) * size + at;
+      auto add = [&](int have) __attribute__((always_inline)) {
+#pragma unroll 16
+        for (int q = 0; q < count; ++q, src += size) {
+          float v[4];
+          read_row<false>(src, 0, have, v);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] += v[e];
+          for (int e = 0; e < 4; ++e) s[e] += v[e];
+        }
+      };
+      if (cols >= 4) add(4);  // no branch between the loads
+      else if (cols > 0) add(cols);
     }
-    write_row<BF16>(static_cast<unsigned char*>(a.dW) + g * size * (BF16 ? 2 : 4), at, cols, s);
-    return;
-  }
-  constexpr int kShares = kJoinThreads / 64;
-  const int w = threadIdx.x >> 6, n = ((int)blockIdx.x - dw_blocks) * 64 + lane;
-  const int64_t per = (pieces + kShares - 1) / kShares;
-  const int64_t q1 = per * (w + 1) < pieces ? per * (w + 1) : pieces;
-  float s = 0.0f;
-  if (n < a.N)
-#pragma unroll 8
-    for (int64_t q = per * w; q < q1; ++q) s += a.db_parts[(first + q) * a.N + n];
-  part[w][lane] = s;
-  __syncthreads();
-  if (w == 0 && n < a.N) {
-#pragma unroll
-    for (int q = 1; q < kShares; ++q) s += part[q][lane];
-    a.db[(int64_t)g * a.N + n] = s;
+    if (shares > 1) {
+      part[w][lane] = make_float4(s[0], s[1], s[2], s[3]);
+      __syncthreads();
+      if (share == 0)
+        for (int q = 1; q < shares; ++q) {
+          const float4 v = part[w + q][lane];
+          s[0] += v.x;
+          s[1] += v.y;
+          s[2] += v.z;
+          s[3] += v.w;
+        }
+      __syncthreads();
+    }
+    if (share == 0 && cols > 0) {
+      if (of_dw)
+        write_row<BF16>(static_cast<unsigned char*>(a.dW) + g * size * (BF16 ? 2 : 4), at, cols, s);
+      else
+        write_row<false>(a.db + (int64_t)g * a.N, at, cols, s);
+    }
   }
 }
 
@@ -660,15 +720,15 @@ hipError_t rows_dtype(const DenseLaunch& a, hipStream_t s) {
 
 // Tiles of dW: the largest of which enough pieces of 512 rows or more (1,024 under
 // 256 x 256) fill the chip.
-inline Shape dw_shape(int64_t n, int N, int K, bool bf16) {
-  if (bf16 && tiles_of(N, K, 256) * (n / 1024) >= 256 && N > 128 && K > 128) return kBig;
+inline Shape dw_shape(int64_t n, int N, int K, int G, bool bf16) {
+  if (bf16 && n >= 4096 * (int64_t)G && tiles_of(N, K, 256) * (n / 1024) >= 256 && N > 128 && K > 128) return kBig;
   return tiles_of(N, K, 128) * (n / 512) >= 256 && N > 64 && K > 64 ? kMid : kSmall;
 }
 
 template <bool BF16>
 hipError_t dw_dtype(const DenseGradLaunch& a, hipStream_t s) {
   using T = Tiles<BF16, true, true>;
-  const Shape shape = dw_shape(a.n, a.N, a.K, BF16);
+  const Shape shape = dw_shape(a.n, a.N, a.K, a.G, BF16);
   if (dw_vectors(a)) {
     if (shape == kSmall) return dw_cfg<typename T::RingSmall>(a, s);
     if (shape == kMid) return dw_cfg<typename T::RingMid>(a, s);
@@ -682,7 +742,7 @@ template <bool BF16>
 bool grads_dtype(const DenseLaunch& x, const DenseGradLaunch& w, hipStream_t s, hipError_t* e) {
   using X = Tiles<BF16, false, true>;
   using W = Tiles<BF16, true, true>;
-  const Shape sx = rows_shape(x, BF16), sw = dw_shape(w.n, w.N, w.K, BF16);
+  const Shape sx = rows_shape(x, BF16), sw = dw_shape(w.n, w.N, w.K, w.G, BF16);
   if (sx == kBig || sw == kBig || !rows_vectors<true>(x) || !dw_vectors(w)) return false;
   if (sx == kSmall && sw == kSmall) *e = grads_cfg<typename X::RingSmall, typename W::RingSmall>(x, w, s);
   else if (sx == kSmall) *e = grads_cfg<typename X::RingSmall, typename W::RingMid>(x, w, s);
@@ -714,8 +774,8 @@ hipError_t launch_dense_rows(const DenseLaunch& a, hipStream_t s) {
 // block of 256 x 256, two of the others), of 256 rows at least. Under more pieces
 // the partial sums cost more than the even ends save (60,000 rows in 64 groups,
 // 512 x 1,024: 960 rows 154 us with the sums, 1,920 rows 127).
-int64_t dense_dw_piece(int64_t n, int N, int K, bool bf16) {
-  const Shape shape = dw_shape(n, N, K, bf16);
+int64_t dense_dw_piece(int64_t n, int N, int K, int G, bool bf16) {
+  const Shape shape = dw_shape(n, N, K, G, bf16);
   const int64_t tiles = tiles_of(N, K, side(shape)), blocks = shape == kBig ? 256 : 512;
   const int64_t want = (blocks + tiles - 1) / tiles;
   const int64_t rows = ((n + want - 1) / want + 63) / 64 * 64;
@@ -726,9 +786,10 @@ hipError_t launch_dense_dz(const DenseGradLaunch& a, hipStream_t s) {
   const int64_t pieces = dense_bias_pieces(a.n, a.offsets ? a.G : 0, a.bias_rows);
   if (pieces <= 0) return hipSuccess;
   ProfileScope prof(kKDenseGrad, s);
+  const int v = a.bf16 ? 8 : 4;
   int lanes = 1;
-  while (lanes < 64 && lanes * 4 < a.N) lanes *= 2;
-  const dim3 grid((unsigned)pieces, (unsigned)((a.N + 4 * lanes - 1) / (4 * lanes)));
+  while (lanes < 64 && lanes * v < a.N) lanes *= 2;
+  const dim3 grid((unsigned)pieces, (unsigned)((a.N + v * lanes - 1) / (v * lanes)));
   if (a.bf16) hipLaunchKernelGGL(dense_dz_kernel<true>, grid, dim3(256), 0, s, a, lanes);
   else hipLaunchKernelGGL(dense_dz_kernel<false>, grid, dim3(256), 0, s, a, lanes);
   return hipGetLastError();
@@ -750,13 +811,28 @@ hipError_t launch_dense_dx_dw(const DenseLaunch& x, const DenseGradLaunch& w, hi
 }
 
 hipError_t launch_dense_join(const DenseGradLaunch& a, hipStream_t s) {
-  const int64_t dw = a.dW && a.dw_parts ? ((int64_t)a.N * a.K + 4 * kJoinThreads - 1) / (4 * kJoinThreads) : 0;
-  const int64_t db = a.db ? (a.N + 63) / 64 : 0;
+  const int64_t groups = a.offsets ? a.G : 1;
+  // Waves per item for a group's usual count of pieces: each then adds about eight.
+  auto shares = [&](int64_t unit) {
+    const int64_t pieces = a.n / groups / unit;
+    return pieces > 32 ? 16 : (pieces > 8 ? 4 : 1);
+  };
+  const int dw_shares = shares(a.piece), db_shares = shares(a.bias_rows);
+  // Groups of more than one piece at most, and two blocks per CU.
+  const int64_t several = std::min(groups, a.n / (a.piece + 1));
+  auto blocks = [](int64_t size, int64_t count, int share) {
+    const int64_t items = (size + 255) / 256 * count, per_block = kJoinWaves / share;
+    return std::min<int64_t>((items + per_block - 1) / per_block, 512);
+  };
+  const int64_t dw = a.dW && a.dw_parts ? blocks((int64_t)a.N * a.K, several, dw_shares) : 0;
+  const int64_t db = a.db ? blocks(a.N, groups, db_shares) : 0;
   if (dw + db == 0) return hipSuccess;
   ProfileScope prof(kKDenseGrad, s);
-  const dim3 grid((unsigned)(dw + db), a.offsets ? a.G : 1);
-  if (a.bf16) hipLaunchKernelGGL(dense_join_kernel<true>, grid, dim3(kJoinThreads), 0, s, a, (int)dw);
-  else hipLaunchKernelGGL(dense_join_kernel<false>, grid, dim3(kJoinThreads), 0, s, a, (int)dw);
+  const dim3 grid((unsigned)(dw + db)), block(64 * kJoinWaves);
+  if (a.bf16)
+    hipLaunchKernelGGL(dense_join_kernel<true>, grid, block, 0, s, a, (int)dw, dw_shares, db_shares);
+  else
+    hipLaunchKernelGGL(dense_join_kernel<false>, grid, block, 0, s, a, (int)dw, dw_shares, db_shares);
   return hipGetLastError();
 }
 

@@ -319,15 +319,15 @@ struct DenseGradLaunch {
   int act;
   bool bf16;
 };
-// 16 to 128, so that blocks of 256 columns make about 1,024.
-inline int dense_bias_rows(int64_t n, int N) {
-  const int64_t rows = n * ((N + 255) / 256) / 1024;
-  return rows >= 128 ? 128 : (rows >= 64 ? 64 : (rows >= 32 ? 32 : 16));
+// 16 to 512, so that there are about 768 blocks (of 256 fp32 or 512 bf16 columns).
+inline int dense_bias_rows(int64_t n, int N, bool bf16) {
+  const int64_t rows = n * (bf16 ? (N + 511) / 512 : (N + 255) / 256) / 768 / 16 * 16 + 16;
+  return rows < 512 ? (int)rows : 512;
 }
 __host__ __device__ inline int64_t dense_bias_pieces(int64_t n, int G, int rows) {
   return (n + rows - 1) / rows + (G ? G + 1 : 0);
 }
-int64_t dense_dw_piece(int64_t n, int N, int K, bool bf16);
+int64_t dense_dw_piece(int64_t n, int N, int K, int G, bool bf16);
 // Partial sums kept at most: only groups of two pieces or more keep any.
 __host__ __device__ inline int64_t dense_dw_parts(int64_t n, int64_t piece, int G) {
   const int64_t pieces = (n + piece - 1) / piece;
