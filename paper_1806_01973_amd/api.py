@@ -509,6 +509,15 @@ class Minibatch:
 NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)  # (a, b, c) of the quintic iteration
 
 
+def _raw_stream(stream: Optional[torch.cuda.Stream], device: torch.device):
+    """The handle of `stream`, or of the device's current one (without building the
+    torch.cuda.Stream object that torch.cuda.current_stream() returns: it takes as long as the
+    smallest of these calls)."""
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
 def _rows(t: torch.Tensor, name: str, n: int, width: int, dtype: torch.dtype) -> int:
     """Checks a matrix [n, width] whose rows are contiguous; returns its row stride."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -581,7 +590,7 @@ def dense_forward(x: torch.Tensor, W: torch.Tensor, b: Optional[torch.Tensor] = 
     st = L.lib().pinsage_dense_forward(ctypes.byref(d), x.data_ptr(), n, ldx,
                                        residual.data_ptr() if residual is not None else None, ldr,
                                        u.data_ptr() if want_preact else None, d.d_out,
-                                       out.data_ptr(), ldy, _stream(stream))
+                                       out.data_ptr(), ldy, _raw_stream(stream, x.device))
     if st:
         L.check(st, "pinsage_dense_forward")
     return (out, u) if want_preact else out
@@ -617,7 +626,8 @@ def dense_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor,
     st = L.lib().pinsage_dense_backward(ctypes.byref(d), dy.data_ptr(), lddy, x.data_ptr(), ldx,
                                         u.data_ptr() if u is not None else None, ldu, n,
                                         _ptr(dx), d.d_in, _ptr(dW), _ptr(db),
-                                        workspace.data_ptr(), workspace.numel(), _stream(stream))
+                                        workspace.data_ptr(), workspace.numel(),
+                                        _raw_stream(stream, x.device))
     if st:
         L.check(st, "pinsage_dense_backward")
     return dx, dW, db
@@ -664,7 +674,8 @@ def orthogonalize(g: torch.Tensor, steps: int = 5, coefficients=NEWTON_SCHULZ, e
     if workspace is None:
         workspace = _newton_schulz_workspace(p, g.device)
     st = L.lib().pinsage_orthogonalize(ctypes.byref(p), g.data_ptr(), out.data_ptr(),
-                                       workspace.data_ptr(), workspace.numel(), _stream(stream))
+                                       workspace.data_ptr(), workspace.numel(),
+                                       _raw_stream(stream, g.device))
     if st:
         L.check(st, "pinsage_orthogonalize")
     return out
@@ -697,7 +708,7 @@ def muon_step(W: torch.Tensor, grad: torch.Tensor, momentum: torch.Tensor, lr: f
     st = L.lib().pinsage_muon_step(ctypes.byref(p), ctypes.byref(m), W.data_ptr(),
                                    grad.data_ptr(), momentum.data_ptr(), W_out.data_ptr(),
                                    momentum_out.data_ptr(), workspace.data_ptr(),
-                                   workspace.numel(), _stream(stream))
+                                   workspace.numel(), _raw_stream(stream, W.device))
     if st:
         L.check(st, "pinsage_muon_step")
     return W_out, momentum_out

@@ -92,6 +92,9 @@ struct Groups {
   int64_t n;
   int unit;
   bool at_least_one, tail;
+  // Blocks take whole pieces before the groups' shorter last ones, and those (up to 64
+  // groups) by descending length: dW's pieces differ by what they sum over.
+  bool longest_first = false;
 
   __device__ __forceinline__ int count() const { return tail ? G + 1 : G; }
   __device__ __forceinline__ void bounds(int g, int64_t& lo, int64_t& hi) const {
@@ -107,49 +110,76 @@ struct Groups {
     return at_least_one && p == 0 ? 1 : p;
   }
   // Piece t, or, given `tiles` per piece, the piece and tile (in t) of block
-  // `block` in an order that keeps neighbouring tiles on one XCD. All lanes of a wave
+  // `block`, neighbouring tiles on one XCD. All lanes of a wave
   // take part; the results are wave-uniform. Up to 64 groups the offsets are read once.
   __device__ __forceinline__ Piece find(int lane, int& t, int block, int tiles) const {
     Piece out;
     const int all = count();
     int64_t lo = 0, hi = 0;
-    int p = 0;
+    int p = 0, whole = 0;
     auto load = [&](int g) __attribute__((always_inline)) {
       lo = hi = 0;
       if (g < all) bounds(g, lo, hi);
       const int q = (int)((hi - lo + unit - 1) / unit);
       p = g < all ? (at_least_one && q == 0 ? 1 : q) : 0;
+      whole = longest_first ? (int)((hi - lo) / unit) : 0;
     };
     load(lane);
-    int incl = wave_inclusive_sum(p, lane);
+    int at = t;
+    int first_whole = 0;  // whole pieces of all groups
     if (tiles > 0) {
-      int total = __builtin_amdgcn_readlane(incl, 63);
+      int total = wave_sum_i32(p);
+      if (longest_first) first_whole = wave_sum_i32(whole);
       for (int g0 = 64; g0 < all; g0 += 64) {
         load(g0 + lane);
         total += wave_sum_i32(p);
+        if (longest_first) first_whole += wave_sum_i32(whole);
       }
-      if (all > 64) {
-        load(lane);
-        incl = wave_inclusive_sum(p, lane);
+      if (all > 64) load(lane);
+      if (longest_first) {
+        // Block b runs on XCD b % 8: a piece's tiles on one of them, the pieces there and
+        // back, so that each XCD has its share of the long ones.
+        const int row = block / 8 / tiles, xcd = block % 8;
+        at = row * 8 + (row & 1 ? 7 - xcd : xcd);
+        t = block / 8 % tiles;
+        if (at >= total) return out;
+      } else {
+        total *= tiles;
+        if (block >= total) return out;
+        at = xcd_tile(block, total);
+        t = at % tiles;
+        at /= tiles;
       }
-      total *= tiles;
-      if (block >= total) return out;
-      const int at = xcd_tile(block, total);
-      t = at % tiles;
-      tiles = at / tiles;  // the piece
-    } else {
-      tiles = t;
+    }
+    // Counted among the whole pieces, or among the others.
+    const bool of_whole = at < first_whole;
+    if (!of_whole) at -= first_whole;
+    if (longest_first && !of_whole && all <= 64) {
+      // The group whose last piece is the at-th longest (ties: the first group).
+      const int rest = p > whole ? (int)((hi - lo) % unit) : -1;
+      int rank = 0;
+      for (int l = 0; l < all; ++l) {
+        const int other = __builtin_amdgcn_readlane(rest, l);
+        rank += other > rest || (other == rest && l < lane);
+      }
+      const unsigned long long hit = __ballot(rest >= 0 && rank == at);
+      const int found = hit ? __builtin_ctzll(hit) : 0;
+      // Its place among the last pieces in group order, which is looked up below.
+      const int order = wave_inclusive_sum(p - whole, lane) - (p - whole);
+      at = __builtin_amdgcn_readlane(order, found);
     }
     int before = 0, slots = 0;
     for (int g0 = 0;;) {
+      const int mine = of_whole ? whole : p - whole;
+      const int incl = wave_inclusive_sum(mine, lane) + before;
       const int slot_incl = wave_inclusive_sum(p > 1 ? p : 0, lane) + slots;
-      incl += before;
-      const unsigned long long past = __ballot(incl > tiles);
+      const unsigned long long past = __ballot(incl > at);
       if (past) {
         const int l = __builtin_ctzll(past);
         out.group = g0 + l;
         out.pieces = __builtin_amdgcn_readlane(p, l);
-        out.index = tiles - (__builtin_amdgcn_readlane(incl, l) - out.pieces);
+        out.index = at - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(mine, l)) +
+                    (of_whole ? 0 : __builtin_amdgcn_readlane(whole, l));
         out.slot = __builtin_amdgcn_readlane(slot_incl, l) - (out.pieces > 1 ? out.pieces : 0);
         out.lo = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(lo >> 32), l) << 32) |
                            (uint32_t)__builtin_amdgcn_readlane((int)lo, l));
@@ -162,7 +192,6 @@ struct Groups {
       g0 += 64;
       if (g0 >= all) return out;
       load(g0 + lane);
-      incl = wave_inclusive_sum(p, lane);
     }
   }
 };
@@ -207,9 +236,23 @@ __device__ __forceinline__ void rows_block(const DenseLaunch& a, int block, int 
   const Operand A{Ap, a.lda, valid, 0};
   const Operand B{Bg + (C::B_COL ? (int64_t)n0 : n0 * a.ldb) * C::ESZ, a.ldb,
                   a.N - n0 < C::BN ? a.N - n0 : C::BN, 0};
-  tile_sums(A, B, 0, orphans ? 0 : a.K, smem, sums);
+  // The residual's tile is touched, a value per 128 bytes, so that it lies in L2 when the
+  // epilogue reads it (60,000 x 1,024 -> 512 bf16: 24 us on top of 73 without).
   const unsigned char* const res =
       a.residual && !orphans ? static_cast<const unsigned char*>(a.residual) : nullptr;
+  constexpr int LINES = C::BN * C::ESZ / 128;
+  constexpr int TOUCHES = (C::BM * LINES + C::THREADS - 1) / C::THREADS;
+  uint32_t touched[TOUCHES] = {};
+  if (res)
+#pragma unroll
+    for (int t = 0; t < TOUCHES; ++t) {
+      const int i = t * C::THREADS + threadIdx.x, m = i / LINES, n = n0 + i % LINES * (128 / C::ESZ);
+      if (m < valid && n < a.N)  // valid <= BM
+        touched[t] = load_any<uint16_t>(res + ((m0 + m) * a.ldr + n) * C::ESZ);
+    }
+  tile_sums(A, B, 0, orphans ? 0 : a.K, smem, sums);
+#pragma unroll
+  for (int t = 0; t < TOUCHES; ++t) asm volatile("" : : "v"(touched[t]));
   struct Row {
     float v[V];
   };
@@ -465,7 +508,7 @@ __device__ __forceinline__ void dw_block(const DenseGradLaunch& a, int block, in
   Piece p;
   int tile = 0;
   if (a.offsets) {
-    p = Groups{a.offsets, a.G, a.n, a.piece, true, false}.find(lane, tile, block, tiles);
+    p = Groups{a.offsets, a.G, a.n, a.piece, true, false, true}.find(lane, tile, block, tiles);
     if (p.group < 0) return;
   } else {
     tile = xcd_tile(block, blocks);
@@ -513,8 +556,10 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void dense_dw_kernel(DenseGradL
   dw_block<C>(a, blockIdx.x, gridDim.x, smem);
 }
 
-// dx and dW in one launch, dW's blocks first: neither fills the chip to its end, and
-// for few rows a launch costs as much as either (about 5 us).
+// dx and dW in one launch, dW's blocks first: for few rows a launch costs as much as
+// either (about 5 us). With many blocks the two only take cache from each other
+// (60,000 x 1,024 -> 512 in 64 equal groups 220 us, apart 108 + 80).
+constexpr int64_t kGradsTogether = 1024;
 template <class CX, class CW>
 __global__ __launch_bounds__(CX::THREADS, CX::WPE) void dense_grads_kernel(DenseLaunch x,
                                                                            DenseGradLaunch w,
@@ -671,7 +716,8 @@ int64_t rows_blocks(const DenseLaunch& a) {
 }
 template <class C>
 int64_t dw_blocks(const DenseGradLaunch& a) {
-  const int64_t pieces = (a.n + a.piece - 1) / a.piece + (a.offsets ? a.G : 0);
+  int64_t pieces = (a.n + a.piece - 1) / a.piece;
+  if (a.offsets) pieces = (pieces + a.G + 7) / 8 * 8;  // as Groups::find hands them out
   return (pieces > 0 ? pieces : 1) * tiles_of(a.N, a.K, C::BM);
 }
 
@@ -693,6 +739,7 @@ template <class CX, class CW>
 hipError_t grads_cfg(const DenseLaunch& x, const DenseGradLaunch& w, hipStream_t s) {
   const int64_t bw = dw_blocks<CW>(w), bx = rows_blocks<CX>(x);
   if (bw + bx > 0x7FFFFFFFll) return hipErrorInvalidValue;
+  if (bw + bx > kGradsTogether) return hipErrorNotReady;  // launched apart
   hipLaunchKernelGGL((dense_grads_kernel<CX, CW>), dim3((unsigned)(bw + bx)), dim3(CX::THREADS), 0, s,
                      x, w, (int)bw);
   return hipGetLastError();
@@ -718,10 +765,12 @@ hipError_t rows_dtype(const DenseLaunch& a, hipStream_t s) {
   return shape == kSmall ? rows_cfg<typename T::Small>(a, s) : rows_cfg<typename T::Mid>(a, s);
 }
 
-// Tiles of dW: the largest of which enough pieces of 512 rows or more (1,024 under
-// 256 x 256) fill the chip.
+// Tiles of dW: 256 x 256 where eight pieces of them fill the chip (the partial sums of
+// more cost what the tile gains), 128 x 128 where pieces of 512 rows or more do.
 inline Shape dw_shape(int64_t n, int N, int K, int G, bool bf16) {
-  if (bf16 && n >= 4096 * (int64_t)G && tiles_of(N, K, 256) * (n / 1024) >= 256 && N > 128 && K > 128) return kBig;
+  const int64_t groups = G ? G : 1;
+  if (bf16 && n >= 4096 * groups && tiles_of(N, K, 256) * groups >= 32 && N > 128 && K > 128)
+    return kBig;
   return tiles_of(N, K, 128) * (n / 512) >= 256 && N > 64 && K > 64 ? kMid : kSmall;
 }
 
@@ -771,12 +820,12 @@ hipError_t launch_dense_rows(const DenseLaunch& a, hipStream_t s) {
 }
 
 // Rows per piece of dW's sums: pieces that give every CU one round of blocks (one
-// block of 256 x 256, two of the others), of 256 rows at least. Under more pieces
-// the partial sums cost more than the even ends save (60,000 rows in 64 groups,
-// 512 x 1,024: 960 rows 154 us with the sums, 1,920 rows 127).
+// block of 256 x 256, two of the others), two rounds with groups, whose sizes are
+// uneven; of 256 rows at least.
 int64_t dense_dw_piece(int64_t n, int N, int K, int G, bool bf16) {
   const Shape shape = dw_shape(n, N, K, G, bf16);
-  const int64_t tiles = tiles_of(N, K, side(shape)), blocks = shape == kBig ? 256 : 512;
+  const int64_t tiles = tiles_of(N, K, side(shape));
+  const int64_t blocks = (shape == kBig ? 256 : 512) * (G > 1 ? 2 : 1);
   const int64_t want = (blocks + tiles - 1) / tiles;
   const int64_t rows = ((n + want - 1) / want + 63) / 64 * 64;
   return rows < 256 ? 256 : rows;
@@ -804,7 +853,9 @@ hipError_t launch_dense_dx_dw(const DenseLaunch& x, const DenseGradLaunch& w, hi
   {
     ProfileScope prof(kKDenseGrad, s);
     hipError_t e = hipSuccess;
-    if (w.bf16 ? grads_dtype<true>(x, w, s, &e) : grads_dtype<false>(x, w, s, &e)) return e;
+    if ((w.bf16 ? grads_dtype<true>(x, w, s, &e) : grads_dtype<false>(x, w, s, &e)) &&
+        e != hipErrorNotReady)
+      return e;
   }
   const hipError_t e = launch_dense_rows(x, s);
   return e != hipSuccess ? e : launch_dense_dw(w, s);
