@@ -8,7 +8,10 @@
 // around a fixed scale 2^12 (values to 16, the smallest normal 2^-26): bf16
 // storage keeps them as one fp16 value each (2^-11 instead of bf16's 2^-8; the
 // result rounds to bf16 once, at the end), fp32 storage as two (22 significand
-// bits, three MFMAs a product, against six for bf16 parts). Sums, and a X, run in
+// bits, three MFMAs a product, against six for bf16 parts). With few singular
+// values the roundings of one part do not average out (error 2.4e-3 on average
+// and 4e-3 at worst for m = 1 .. 16, against 1.7e-3 of bf16's own and 2.2e-3 in all
+// for m >= 100), so up to 64 bf16 storage takes two parts as well. Sums, and a X, run in
 // fp32; |G|_F is summed in fp64, so no finite G overflows.
 // X, its transpose T, A and B live in the workspace, padded with zeros to whole
 // tiles, so that no product has an edge and each reads both operands along k:
@@ -32,6 +35,7 @@ struct NewtonWork {
   int m, n, mp, np;  // m <= n; padded
   int norm_blocks;
   bool flip;         // X is G^T
+  bool two;          // two fp16 parts
 };
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -120,9 +124,8 @@ __global__ __launch_bounds__(256) void newton_norm_kernel(NewtonLaunch a, Newton
 }
 
 // ---- X0 and its transpose: scaled, in fp16 parts, padded --------------------------
-template <bool BF16>
+template <bool BF16, int PLANES>
 __global__ __launch_bounds__(256) void newton_start_kernel(NewtonLaunch a, NewtonWork w) {
-  constexpr int PLANES = BF16 ? 1 : 2;
   __shared__ float tile[64][65];
   __shared__ double part[4];
   const int tid = threadIdx.x;
@@ -284,18 +287,244 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch
   }
 }
 
+// ---- small matrices: everything in one block ------------------------------------------
+// A block of eight waves takes a matrix from G to the result, X and one m x m matrix in
+// its LDS: what bounds the launches above for small matrices is that there are 17 of
+// them, at 3 to 5 us each whatever they compute. In two parts always. Up to 64 x 384, and
+// in fp32 128 x 128, measured, us, one block / launches: 64 x 64 26 / 59 (bf16 53), 512 of
+// them 54 / 113, 300 x 40 50 / 75, 128 x 128 72 / 79 (bf16 64), 64 x 512 98 / 84.
+// X [mp][np] and A [mp][mp] lie in LDS in fp16 parts, 16-byte slot s of row r at
+// s ^ small_swizzle(r): a fragment read's 8 rows, and the 4 rows of a transposing read
+// (X's columns, for B X), fall on distinct banks. A wave's blocks of 32 x 32 stay in its
+// accumulators until all waves have read what they replace.
+constexpr int kSmallWaves = 8, kSmallBlocks = 3;  // blocks per wave at most, of X or A
+constexpr int kSmallLds = 128 * 1024;
+
+__device__ __forceinline__ int small_swizzle(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
+
+inline bool fits_one_block(const NewtonWork& w, bool bf16) {
+  return (w.mp == 64 && w.np <= 384) || (!bf16 && w.mp == 128 && w.np == 128);
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLaunch a,
+                                                                        NewtonWork w) {
+  constexpr int PLANES = 2, MODE = kF16x2, THREADS = 64 * kSmallWaves;
+  __shared__ __attribute__((aligned(16))) unsigned char smem[kSmallLds];
+  __shared__ double norms[kSmallWaves];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int mp = w.mp, np = w.np, mb = mp / 32, nb = np / 32;
+  const int64_t size = (int64_t)a.rows * a.cols, base = blockIdx.x * size;
+  unsigned char* const X = smem;                          // planes of mp rows of np
+  unsigned char* const A = smem + PLANES * mp * np * 2;   // planes of mp rows of mp
+  const int px = mp * np * 2, pa = mp * mp * 2;
+
+  // The norm, with the momentum's update.
+  double s = 0.0;
+  const int cells = (a.cols + 3) / 4;  // of four elements of a row
+  for (int q = tid; q < a.rows * cells; q += THREADS) {
+    const int r = q / cells, c = q % cells * 4, cols = a.cols - c;
+    const int64_t at = base + (int64_t)r * a.cols + c;
+    float u[4];
+    read_row<BF16>(a.in, at, cols, u);
+    if (a.weight) {
+      float m[4];
+      read_row<false>(a.momentum, at, cols, m);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        m[e] = fmaf(a.beta, m[e], u[e]);
+        u[e] = a.nesterov ? fmaf(a.beta, m[e], u[e]) : m[e];
+      }
+      write_row<false>(a.momentum_out, at, cols, m);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s = e < cols ? fma((double)u[e], (double)u[e], s) : s;
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o);
+  if (lane == 0) norms[wave] = s;
+  // X's padding.
+  for (int q = tid; q < PLANES * mp * np / 8; q += THREADS)
+    reinterpret_cast<u32x4*>(X)[q] = u32x4{0, 0, 0, 0};
+  __syncthreads();
+  s = 0.0;
+#pragma unroll
+  for (int q = 0; q < kSmallWaves; ++q) s += norms[q];
+  const double inv = (double)kScale / (sqrt(s) + (double)a.eps);
+
+  // X0; a thread reads what it wrote of the momentum.
+  for (int q = tid; q < a.rows * cells; q += THREADS) {
+    const int r = q / cells, c = q % cells * 4, cols = a.cols - c;
+    float u[4];
+    update4<BF16>(a, base + (int64_t)r * a.cols + c, cols, u);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (e >= cols) break;
+      const int i = w.flip ? c + e : r, j = w.flip ? r : c + e;
+      unsigned char* const to = X + i * np * 2 + (((j >> 3) ^ small_swizzle(i)) * 16) + (j & 7) * 2;
+      const float v = (float)(u[e] * inv);
+      const _Float16 hi = (_Float16)v;
+      *reinterpret_cast<_Float16*>(to) = hi;
+      if constexpr (PLANES == 2) *reinterpret_cast<_Float16*>(to + px) = (_Float16)(v - (float)hi);
+    }
+  }
+  __syncthreads();
+
+  const int frag_row = lane & 31, half = lane >> 5;
+  struct Frag {
+    u32x4 p[PLANES];
+  };
+  auto row_frag = [&](const unsigned char* M, int pitch, int plane, int r0, int ks)
+      __attribute__((always_inline)) {
+    Frag f;
+    const int r = r0 + frag_row;
+#pragma unroll
+    for (int p = 0; p < PLANES; ++p)
+      f.p[p] = *reinterpret_cast<const u32x4*>(M + p * plane + r * pitch +
+                                               (((2 * ks + half) ^ small_swizzle(r)) * 16));
+    return f;
+  };
+  // Columns c0 .. c0 + 31 of X, k along its rows.
+  auto col_frag = [&](int c0, int ks) __attribute__((always_inline)) {
+    Frag f;
+    const int c = c0 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+#pragma unroll
+    for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int k = 16 * ks + 8 * half + 4 * h + ((lane >> 2) & 3);
+        const unsigned char* const at =
+            X + p * px + k * np * 2 + (((c >> 3) ^ small_swizzle(k)) * 16) + (c & 4) * 2;
+        const u32x2 x = __builtin_bit_cast(
+            u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                       (__attribute__((address_space(3))) s16x4*)at));
+        f.p[p][2 * h] = x[0];
+        f.p[p][2 * h + 1] = x[1];
+      }
+    return f;
+  };
+  auto multiply = [&](const Frag& b, const Frag& l, f32x16& acc) __attribute__((always_inline)) {
+    if constexpr (PLANES == 2) {
+      acc = product_mfma<MODE>(b.p[PLANES - 1], l.p[0], acc);
+      acc = product_mfma<MODE>(b.p[0], l.p[PLANES - 1], acc);
+    }
+    acc = product_mfma<MODE>(b.p[0], l.p[0], acc);
+  };
+  // Block (bi, bj) of M becomes p M + q sum.
+  auto update = [&](unsigned char* M, int pitch, int plane, int bi, int bj, float p, float q,
+                    const f32x16& sum) __attribute__((always_inline)) {
+    const int i = 32 * bi + frag_row;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int j = 32 * bj + 8 * g + 4 * half;
+      uint16_t* const at = reinterpret_cast<uint16_t*>(
+          M + i * pitch + (((j >> 3) ^ small_swizzle(i)) * 16) + (j & 4) * 2);
+      float v[4];
+      if (p == 0.0f) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = q * sum[4 * g + e];
+      } else {
+        const uint2 hi = *reinterpret_cast<const uint2*>(at);
+        uint2 lo = make_uint2(0, 0);
+        if constexpr (PLANES == 2) lo = *reinterpret_cast<const uint2*>(at + plane / 2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t h = e < 2 ? hi.x : hi.y, l = e < 2 ? lo.x : lo.y;
+          float old = unpack_f16(h, e & 1);
+          if constexpr (PLANES == 2) old += unpack_f16(l, e & 1);
+          v[e] = fmaf(p, old, q * sum[4 * g + e]);
+        }
+      }
+      put<PLANES>(at, plane / 2, v);
+    }
+  };
+  const float back = 1.0f / kScale;  // products carry the scale twice
+  f32x16 acc[kSmallBlocks];
+
+  for (int step = 0; step < a.steps; ++step) {
+    // A = X X^T, a wave's blocks in turn.
+    for (int b = wave; b < mb * mb; b += kSmallWaves) {
+      const int bi = b / mb, bj = b % mb;
+      clear_block(acc[0]);
+      for (int ks = 0; ks < np / 16; ++ks)
+        multiply(row_frag(X, np * 2, px, 32 * bj, ks), row_frag(X, np * 2, px, 32 * bi, ks), acc[0]);
+      update(A, mp * 2, pa, bi, bj, 0.0f, back, acc[0]);
+    }
+    __syncthreads();
+    // A becomes b A + c A A (A is symmetric: both operands are its rows).
+#pragma unroll
+    for (int t = 0; t < kSmallBlocks; ++t) clear_block(acc[t]);
+    for (int ks = 0; ks < mp / 16; ++ks)
+#pragma unroll
+      for (int t = 0; t < kSmallBlocks; ++t) {
+        const int b = wave + t * kSmallWaves;
+        if (b < mb * mb)
+          multiply(row_frag(A, mp * 2, pa, 32 * (b % mb), ks),
+                   row_frag(A, mp * 2, pa, 32 * (b / mb), ks), acc[t]);
+      }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < kSmallBlocks; ++t) {
+      const int b = wave + t * kSmallWaves;
+      if (b < mb * mb) update(A, mp * 2, pa, b / mb, b % mb, a.b, a.c * back, acc[t]);
+    }
+    __syncthreads();
+    // X becomes a X + A X.
+#pragma unroll
+    for (int t = 0; t < kSmallBlocks; ++t) clear_block(acc[t]);
+    for (int ks = 0; ks < mp / 16; ++ks)
+#pragma unroll
+      for (int t = 0; t < kSmallBlocks; ++t) {
+        const int b = wave + t * kSmallWaves;
+        if (b < mb * nb)
+          multiply(col_frag(32 * (b / mb), ks), row_frag(A, mp * 2, pa, 32 * (b % mb), ks), acc[t]);
+      }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < kSmallBlocks; ++t) {
+      const int b = wave + t * kSmallWaves;
+      if (b < mb * nb) update(X, np * 2, px, b % mb, b / mb, a.a, back, acc[t]);
+    }
+    __syncthreads();
+  }
+
+  // The result, along G's rows.
+  for (int q = tid; q < a.rows * cells; q += THREADS) {
+    const int r = q / cells, c = q % cells * 4, cols = a.cols - c;
+    const int64_t at = base + (int64_t)r * a.cols + c;
+    float v[4], old[4] = {};
+    if (a.weight) read_row<BF16>(a.weight, at, cols, old);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = w.flip ? c + e : r, j = w.flip ? r : c + e;
+      v[e] = 0.0f;
+      if (e < cols) {
+        const unsigned char* const from =
+            X + i * np * 2 + (((j >> 3) ^ small_swizzle(i)) * 16) + (j & 7) * 2;
+        v[e] = (float)*reinterpret_cast<const _Float16*>(from);
+        if constexpr (PLANES == 2) v[e] += (float)*reinterpret_cast<const _Float16*>(from + px);
+      }
+      v[e] *= back;
+      if (a.weight) v[e] = fmaf(a.decay, old[e], -a.rate * v[e]);
+    }
+    write_row<BF16>(a.out, at, cols, v);
+  }
+}
+
 // ---- tile shapes --------------------------------------------------------------------
 // Measured at depth 2,048, us (fp16): 64 x 64 tiles with four stages, two blocks per
 // CU, 10.8 at 256 tiles and 23.8 at 529; with two stages, which more of them share a
 // CU, 18.4, 20.8 and 27.8 at 1,024; 128 x 128 with four stages 23.9 at 256 tiles (as
 // 1,024 of 64 x 64), with two 28.2, but 75 against 103 at 1,876 tiles of depth 1,024.
-// Two parts: 64 x 64 59.6 at 1,024 tiles, 128 x 128 57.0.
+// Two parts: 64 x 64 with four stages 19.3 at 256 tiles, with two 24.3 and 59.6 at
+// 1,024, 128 x 128 57.0.
 inline int64_t tiles_of(const NewtonWork& w, int64_t batch, bool symmetric, int side) {
   const int64_t tm = (w.mp + side - 1) / side, tn = (w.np + side - 1) / side;
   return (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batch;
 }
-inline bool small_tiles(const NewtonWork& w, int64_t batch, bool symmetric, bool bf16) {
-  return tiles_of(w, batch, symmetric, 64) <= (bf16 ? 768 : 1024);
+inline bool small_tiles(const NewtonWork& w, int64_t batch, bool symmetric) {
+  return tiles_of(w, batch, symmetric, 64) <= (w.two ? 1024 : 768);
 }
 
 template <class C, int KIND, bool BF16>
@@ -305,24 +534,26 @@ void launch_one(const NewtonLaunch& a, const NewtonWork& w, int from, hipStream_
                      dim3(C::THREADS), 0, s, a, w, from);
 }
 
-template <int KIND, bool BF16>
+template <int KIND, bool BF16, int PLANES>
 void launch_product(const NewtonLaunch& a, const NewtonWork& w, int from, hipStream_t s) {
   constexpr bool kSymmetric = KIND == kGram || KIND == kSquare;
-  const bool small = small_tiles(w, a.batch, kSymmetric, BF16);
-  if constexpr (BF16) {
+  const bool small = small_tiles(w, a.batch, kSymmetric);
+  if constexpr (PLANES == 1) {
     if (small && tiles_of(w, a.batch, kSymmetric, 64) <= 512)
-      launch_one<RingCfg<kF16, 64, 64, 64, 2, 2, false, false, 4>, KIND, true>(a, w, from, s);
+      launch_one<RingCfg<kF16, 64, 64, 64, 2, 2, false, false, 4>, KIND, BF16>(a, w, from, s);
     else if (small)
-      launch_one<RingCfg<kF16, 64, 64, 64, 2, 2, false, false, 2>, KIND, true>(a, w, from, s);
+      launch_one<RingCfg<kF16, 64, 64, 64, 2, 2, false, false, 2>, KIND, BF16>(a, w, from, s);
     else if (tiles_of(w, a.batch, kSymmetric, 128) <= 256)
-      launch_one<RingCfg<kF16, 128, 128, 64, 2, 2, false, false, 4>, KIND, true>(a, w, from, s);
+      launch_one<RingCfg<kF16, 128, 128, 64, 2, 2, false, false, 4>, KIND, BF16>(a, w, from, s);
     else
-      launch_one<RingCfg<kF16, 128, 128, 64, 2, 2, false, false, 2>, KIND, true>(a, w, from, s);
+      launch_one<RingCfg<kF16, 128, 128, 64, 2, 2, false, false, 2>, KIND, BF16>(a, w, from, s);
   } else {
-    if (small)
-      launch_one<RingCfg<kF16x2, 64, 64, 64, 2, 2, false, false, 2>, KIND, false>(a, w, from, s);
+    if (small && tiles_of(w, a.batch, kSymmetric, 64) <= 256)
+      launch_one<RingCfg<kF16x2, 64, 64, 64, 2, 2, false, false, 4>, KIND, BF16>(a, w, from, s);
+    else if (small)
+      launch_one<RingCfg<kF16x2, 64, 64, 64, 2, 2, false, false, 2>, KIND, BF16>(a, w, from, s);
     else
-      launch_one<RingCfg<kF16x2, 128, 128, 32, 2, 2, false, false, 4>, KIND, false>(a, w, from, s);
+      launch_one<RingCfg<kF16x2, 128, 128, 32, 2, 2, false, false, 4>, KIND, BF16>(a, w, from, s);
   }
 }
 
@@ -332,15 +563,16 @@ size_t layout(int64_t batch, int rows, int cols, bool bf16, unsigned char* ws, N
   w->flip = rows > cols;
   w->m = w->flip ? cols : rows;
   w->n = w->flip ? rows : cols;
+  w->two = !bf16 || w->m <= 64;
   w->mp = (w->m + 63) / 64 * 64;
   w->np = (w->n + 63) / 64 * 64;
-  if (!small_tiles(*w, batch, true, bf16) || !small_tiles(*w, batch, false, bf16)) {
+  if (!small_tiles(*w, batch, true) || !small_tiles(*w, batch, false)) {
     w->mp = (w->m + 127) / 128 * 128;
     w->np = (w->n + 127) / 128 * 128;
   }
   const int64_t blocks = ((int64_t)rows * cols + 4095) / 4096;
   w->norm_blocks = (int)(blocks < kMaxNormBlocks ? blocks : kMaxNormBlocks);
-  const size_t planes = bf16 ? 1 : 2;
+  const size_t planes = w->two ? 2 : 1;
   const size_t x = aligned((size_t)batch * planes * w->mp * w->np * 2);
   const size_t g = aligned((size_t)batch * planes * w->mp * w->mp * 2);
   const size_t norms = aligned((size_t)batch * kMaxNormBlocks * sizeof(double));
@@ -355,18 +587,32 @@ size_t layout(int64_t batch, int rows, int cols, bool bf16, unsigned char* ws, N
   return norms + 4 * x + 2 * g;
 }
 
-template <bool BF16>
-hipError_t launch_dtype(const NewtonLaunch& a, const NewtonWork& w, hipStream_t s) {
+// The padded sides of a small matrix, whatever its batch asks of the launches.
+bool one_block(const NewtonLaunch& a, NewtonWork* w) {
+  NewtonWork one = *w;
+  one.mp = (w->m + 63) / 64 * 64;
+  one.np = (w->n + 63) / 64 * 64;
+  if (!fits_one_block(one, a.bf16)) return false;
+  *w = one;
+  return true;
+}
+
+template <bool BF16, int PLANES>
+hipError_t launch_parts(const NewtonLaunch& a, NewtonWork w, hipStream_t s) {
   const unsigned batch = (unsigned)a.batch;
+  if (one_block(a, &w)) {
+    hipLaunchKernelGGL(newton_small_kernel<BF16>, dim3(batch), dim3(64 * kSmallWaves), 0, s, a, w);
+    return hipGetLastError();
+  }
   hipLaunchKernelGGL(newton_norm_kernel<BF16>, dim3((unsigned)w.norm_blocks, batch), dim3(256), 0, s,
                      a, w);
-  hipLaunchKernelGGL(newton_start_kernel<BF16>,
+  hipLaunchKernelGGL((newton_start_kernel<BF16, PLANES>),
                      dim3((unsigned)(w.np / 64), (unsigned)(w.mp / 64), batch), dim3(256), 0, s, a, w);
   for (int k = 0, from = 0; k < a.steps; ++k, from = 1 - from) {
-    launch_product<kGram, BF16>(a, w, from, s);
-    launch_product<kSquare, BF16>(a, w, from, s);
-    if (k + 1 < a.steps) launch_product<kApply, BF16>(a, w, from, s);
-    else launch_product<kLast, BF16>(a, w, from, s);
+    launch_product<kGram, BF16, PLANES>(a, w, from, s);
+    launch_product<kSquare, BF16, PLANES>(a, w, from, s);
+    if (k + 1 < a.steps) launch_product<kApply, BF16, PLANES>(a, w, from, s);
+    else launch_product<kLast, BF16, PLANES>(a, w, from, s);
   }
   return hipGetLastError();
 }
@@ -383,7 +629,8 @@ hipError_t launch_newton(const NewtonLaunch& a, void* workspace, hipStream_t s) 
   ProfileScope prof(kKNewtonSchulz, s);
   NewtonWork w;
   layout(a.batch, a.rows, a.cols, a.bf16, static_cast<unsigned char*>(workspace), &w);
-  return a.bf16 ? launch_dtype<true>(a, w, s) : launch_dtype<false>(a, w, s);
+  if (!a.bf16) return launch_parts<false, 2>(a, w, s);
+  return w.two ? launch_parts<true, 2>(a, w, s) : launch_parts<true, 1>(a, w, s);
 }
 
 }  // namespace pinsage
