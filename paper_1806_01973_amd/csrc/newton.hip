@@ -13,10 +13,10 @@
 // and 4e-3 at worst for m = 1 .. 16, against 1.7e-3 of bf16's own and 2.2e-3 in all
 // for m >= 100), so up to 64 bf16 storage takes two parts as well. Sums, and a X, run in
 // fp32; |G|_F is summed in fp64, so no finite G overflows.
-// X, its transpose T, A and B live in the workspace, padded with zeros to whole
-// tiles, so that no product has an edge and each reads both operands along k:
-// A = X X^T, A A^T, and B T^T. A and A A are symmetric: only their tiles on and
-// above the diagonal are computed, and stored twice.
+// Y = X^T, A and B live in the workspace, padded with zeros to whole tiles, so that
+// no product has an edge: A = Y^T Y (both operands by columns), A A, and
+// Y = a Y + Y B. A and A A are symmetric: only their tiles on and above the diagonal
+// are computed, and stored twice.
 #include "kernels.h"
 #include "ring_device.h"
 
@@ -24,12 +24,11 @@ namespace pinsage {
 namespace {
 
 constexpr float kScale = 4096.0f;  // the stored values over the true ones
-constexpr int kMaxNormBlocks = 256;  // partial sums of a matrix's norm
+constexpr int kMaxNormBlocks = 1024;  // partial sums of a matrix's norm
 
 struct NewtonWork {
   double* norms;     // [batch][kMaxNormBlocks]
-  uint16_t* X[2];    // [batch][planes][mp][np]
-  uint16_t* T[2];    // [batch][planes][np][mp]
+  uint16_t* Y[2];    // [batch][planes][np][mp]
   uint16_t* A;       // [batch][planes][mp][mp]
   uint16_t* B;
   int m, n, mp, np;  // m <= n; padded
@@ -123,13 +122,15 @@ __global__ __launch_bounds__(256) void newton_norm_kernel(NewtonLaunch a, Newton
     w.norms[blockIdx.y * kMaxNormBlocks + blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// ---- X0 and its transpose: scaled, in fp16 parts, padded --------------------------
+// ---- Y0: scaled, in fp16 parts, padded ---------------------------------------------
 template <bool BF16, int PLANES>
 __global__ __launch_bounds__(256) void newton_start_kernel(NewtonLaunch a, NewtonWork w) {
   __shared__ float tile[64][65];
   __shared__ double part[4];
   const int tid = threadIdx.x;
-  double s = tid < w.norm_blocks ? w.norms[(int64_t)blockIdx.z * kMaxNormBlocks + tid] : 0.0;
+  double s = 0.0;
+  for (int q = tid; q < w.norm_blocks; q += 256)
+    s += w.norms[(int64_t)blockIdx.z * kMaxNormBlocks + q];
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o);
   if ((tid & 63) == 0) part[tid >> 6] = s;
@@ -137,8 +138,8 @@ __global__ __launch_bounds__(256) void newton_start_kernel(NewtonLaunch a, Newto
   s = (part[0] + part[1]) + (part[2] + part[3]);
   const double inv = (double)kScale / (sqrt(s) + (double)a.eps);
   const int64_t base = (int64_t)blockIdx.z * a.rows * a.cols;
-  const int r0 = (w.flip ? blockIdx.x : blockIdx.y) * 64;  // of G
-  const int c0 = (w.flip ? blockIdx.y : blockIdx.x) * 64;
+  const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;              // of Y
+  const int r0 = w.flip ? i0 : j0, c0 = w.flip ? j0 : i0;  // of G
 #pragma unroll
   for (int q = tid; q < 64 * 16; q += 256) {
     const int r = q / 16, c = q % 16 * 4, cols = a.cols - c0 - c;
@@ -149,29 +150,22 @@ __global__ __launch_bounds__(256) void newton_start_kernel(NewtonLaunch a, Newto
     for (int e = 0; e < 4; ++e) tile[r][c + e] = (float)(u[e] * inv);
   }
   __syncthreads();
-  // The tile as it lies goes to X, or to T when X is G^T; turned, to the other.
   const int64_t plane = (int64_t)w.mp * w.np;
-  uint16_t* const along = (w.flip ? w.T[0] : w.X[0]) + blockIdx.z * PLANES * plane;
-  uint16_t* const across = (w.flip ? w.X[0] : w.T[0]) + blockIdx.z * PLANES * plane;
-  const int64_t lda = w.flip ? w.mp : w.np, ldx = w.flip ? w.np : w.mp;
+  uint16_t* const Y = w.Y[0] + blockIdx.z * PLANES * plane;
 #pragma unroll
   for (int q = tid; q < 64 * 8; q += 256) {
     const int i = q / 8, j = q % 8 * 8;
-    float v[8], t[8];
+    float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      v[e] = tile[i][j + e];
-      t[e] = tile[j + e][i];
-    }
-    put<PLANES>(along + (int64_t)(r0 + i) * lda + c0 + j, plane, v);
-    put<PLANES>(across + (int64_t)(c0 + i) * ldx + r0 + j, plane, t);
+    for (int e = 0; e < 8; ++e) v[e] = w.flip ? tile[i][j + e] : tile[j + e][i];
+    put<PLANES>(Y + (int64_t)(i0 + i) * w.mp + j0 + j, plane, v);
   }
 }
 
 // ---- the three products -----------------------------------------------------------
 enum NewtonProduct { kGram = 0, kSquare = 1, kApply = 2, kLast = 3 };
 
-// P[i][j] = sum_k L[i][k] R[j][k]: X X^T, A A (A is symmetric), or B X = B (X^T)^T.
+// P[i][j] = sum_k L(i, k) R(j, k): Y^T Y, A A, or Y B (A and B are symmetric).
 template <class C, int KIND, bool BF16>
 __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch a, NewtonWork w,
                                                                     int from) {
@@ -179,7 +173,7 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch
   constexpr int PLANES = C::MEM_PLANES;
   constexpr bool kSymmetric = KIND == kGram || KIND == kSquare;
   const int64_t px = (int64_t)w.mp * w.np, pa = (int64_t)w.mp * w.mp, z = blockIdx.y;
-  const uint16_t* const X = w.X[from] + z * PLANES * px;
+  const uint16_t* const Y = w.Y[from] + z * PLANES * px;
   uint16_t* const A = w.A + z * PLANES * pa;
   uint16_t* const B = w.B + z * PLANES * pa;
   int ti, tj;
@@ -191,7 +185,7 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch
     while (left >= T - ti) left -= T - ti++;
     tj = ti + left;
   } else {
-    const int T = w.np / C::BN;
+    const int T = w.mp / C::BN;
     ti = blockIdx.x / T;
     tj = blockIdx.x % T;
   }
@@ -199,16 +193,13 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch
   Operand L, R;
   int depth;
   if constexpr (KIND == kGram) {
-    L = Operand{X + (int64_t)i0 * w.np, w.np, C::BM, px * 2};
-    R = Operand{X + (int64_t)j0 * w.np, w.np, C::BN, px * 2};
+    L = Operand{Y + i0, w.mp, C::BM, px * 2};
+    R = Operand{Y + j0, w.mp, C::BN, px * 2};
     depth = w.np;
-  } else if constexpr (KIND == kSquare) {
-    L = Operand{A + (int64_t)i0 * w.mp, w.mp, C::BM, pa * 2};
-    R = Operand{A + (int64_t)j0 * w.mp, w.mp, C::BN, pa * 2};
-    depth = w.mp;
   } else {
-    L = Operand{B + (int64_t)i0 * w.mp, w.mp, C::BM, pa * 2};
-    R = Operand{w.T[from] + z * PLANES * px + (int64_t)j0 * w.mp, w.mp, C::BN, px * 2};
+    L = Operand{(KIND == kSquare ? A : Y) + (int64_t)i0 * w.mp, w.mp, C::BM,
+                (KIND == kSquare ? pa : px) * 2};
+    R = Operand{(KIND == kSquare ? A : B) + (int64_t)j0 * w.mp, w.mp, C::BN, pa * 2};
     depth = w.mp;
   }
   TileSums<C> sums;
@@ -237,22 +228,18 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch
         },
         ti != tj);
   } else if constexpr (KIND == kApply) {
-    uint16_t* const outx = w.X[1 - from] + z * PLANES * px;
-    uint16_t* const outt = w.T[1 - from] + z * PLANES * px;
+    uint16_t* const out = w.Y[1 - from] + z * PLANES * px;
     product_rows_cols<8>(
         sums, smem,
         [&](int m, int n) __attribute__((always_inline)) {
-          return get8<PLANES>(X + (int64_t)(i0 + m) * w.np + j0 + n, px);
+          return get8<PLANES>(Y + (int64_t)(i0 + m) * w.mp + j0 + n, px);
         },
         [&](int m, int n, float (&v)[8], const auto& x) __attribute__((always_inline)) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] = fmaf(a.a, value(x, e), back * v[e]);
-          put<PLANES>(outx + (int64_t)(i0 + m) * w.np + j0 + n, px, v);
+          put<PLANES>(out + (int64_t)(i0 + m) * w.mp + j0 + n, px, v);
         },
-        [&](int m, int n, const float (&v)[8]) __attribute__((always_inline)) {
-          put<PLANES>(outt + (int64_t)(j0 + n) * w.mp + i0 + m, px, v);
-        },
-        true);
+        [](int, int, const float (&)[8]) {}, false);
   } else {
     const int64_t base = z * a.rows * a.cols;
     // Up to eight results of one row of G, from `at` on.
@@ -268,22 +255,22 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch
     product_rows_cols<8>(
         sums, smem,
         [&](int m, int n) __attribute__((always_inline)) {
-          return get8<PLANES>(X + (int64_t)(i0 + m) * w.np + j0 + n, px);
+          return get8<PLANES>(Y + (int64_t)(i0 + m) * w.mp + j0 + n, px);
         },
         [&](int m, int n, float (&v)[8], const auto& x) __attribute__((always_inline)) {
           const int i = i0 + m, j = j0 + n;
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] = fmaf(a.a, value(x, e), back * v[e]) * back;
-          if (!w.flip && i < w.m && j < w.n) give(base + (int64_t)i * a.cols + j, w.n - j, v);
+          if (w.flip && i < w.n && j < w.m) give(base + (int64_t)i * a.cols + j, w.m - j, v);
         },
         [&](int m, int n, const float (&v)[8]) __attribute__((always_inline)) {
           const int i = i0 + m, j = j0 + n;
           float y[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) y[e] = v[e];
-          if (i < w.m && j < w.n) give(base + (int64_t)j * a.cols + i, w.m - i, y);
+          if (i < w.n && j < w.m) give(base + (int64_t)j * a.cols + i, w.n - i, y);
         },
-        w.flip);
+        !w.flip);
   }
 }
 
@@ -536,24 +523,24 @@ void launch_one(const NewtonLaunch& a, const NewtonWork& w, int from, hipStream_
 
 template <int KIND, bool BF16, int PLANES>
 void launch_product(const NewtonLaunch& a, const NewtonWork& w, int from, hipStream_t s) {
-  constexpr bool kSymmetric = KIND == kGram || KIND == kSquare;
+  constexpr bool kSymmetric = KIND == kGram || KIND == kSquare, kCol = KIND == kGram;
   const bool small = small_tiles(w, a.batch, kSymmetric);
   if constexpr (PLANES == 1) {
     if (small && tiles_of(w, a.batch, kSymmetric, 64) <= 512)
-      launch_one<RingCfg<kF16, 64, 64, 64, 2, 2, false, false, 4>, KIND, BF16>(a, w, from, s);
+      launch_one<RingCfg<kF16, 64, 64, 64, 2, 2, kCol, kCol, 4>, KIND, BF16>(a, w, from, s);
     else if (small)
-      launch_one<RingCfg<kF16, 64, 64, 64, 2, 2, false, false, 2>, KIND, BF16>(a, w, from, s);
+      launch_one<RingCfg<kF16, 64, 64, 64, 2, 2, kCol, kCol, 2>, KIND, BF16>(a, w, from, s);
     else if (tiles_of(w, a.batch, kSymmetric, 128) <= 256)
-      launch_one<RingCfg<kF16, 128, 128, 64, 2, 2, false, false, 4>, KIND, BF16>(a, w, from, s);
+      launch_one<RingCfg<kF16, 128, 128, 64, 2, 2, kCol, kCol, 4>, KIND, BF16>(a, w, from, s);
     else
-      launch_one<RingCfg<kF16, 128, 128, 64, 2, 2, false, false, 2>, KIND, BF16>(a, w, from, s);
+      launch_one<RingCfg<kF16, 128, 128, 64, 2, 2, kCol, kCol, 2>, KIND, BF16>(a, w, from, s);
   } else {
     if (small && tiles_of(w, a.batch, kSymmetric, 64) <= 256)
-      launch_one<RingCfg<kF16x2, 64, 64, 64, 2, 2, false, false, 4>, KIND, BF16>(a, w, from, s);
+      launch_one<RingCfg<kF16x2, 64, 64, 64, 2, 2, kCol, kCol, 4>, KIND, BF16>(a, w, from, s);
     else if (small)
-      launch_one<RingCfg<kF16x2, 64, 64, 64, 2, 2, false, false, 2>, KIND, BF16>(a, w, from, s);
+      launch_one<RingCfg<kF16x2, 64, 64, 64, 2, 2, kCol, kCol, 2>, KIND, BF16>(a, w, from, s);
     else
-      launch_one<RingCfg<kF16x2, 128, 128, 32, 2, 2, false, false, 4>, KIND, BF16>(a, w, from, s);
+      launch_one<RingCfg<kF16x2, 128, 128, 32, 2, 2, kCol, kCol, 4>, KIND, BF16>(a, w, from, s);
   }
 }
 
@@ -578,13 +565,11 @@ size_t layout(int64_t batch, int rows, int cols, bool bf16, unsigned char* ws, N
   const size_t norms = aligned((size_t)batch * kMaxNormBlocks * sizeof(double));
   w->norms = reinterpret_cast<double*>(ws);
   uint16_t* const rest = reinterpret_cast<uint16_t*>(ws + norms);
-  w->X[0] = rest;
-  w->X[1] = rest + x / 2;
-  w->T[0] = rest + x;
-  w->T[1] = rest + x / 2 * 3;
-  w->A = rest + x * 2;
-  w->B = rest + x * 2 + g / 2;
-  return norms + 4 * x + 2 * g;
+  w->Y[0] = rest;
+  w->Y[1] = rest + x / 2;
+  w->A = rest + x;
+  w->B = rest + x + g / 2;
+  return norms + 2 * x + 2 * g;
 }
 
 // The padded sides of a small matrix, whatever its batch asks of the launches.
@@ -607,7 +592,7 @@ hipError_t launch_parts(const NewtonLaunch& a, NewtonWork w, hipStream_t s) {
   hipLaunchKernelGGL(newton_norm_kernel<BF16>, dim3((unsigned)w.norm_blocks, batch), dim3(256), 0, s,
                      a, w);
   hipLaunchKernelGGL((newton_start_kernel<BF16, PLANES>),
-                     dim3((unsigned)(w.np / 64), (unsigned)(w.mp / 64), batch), dim3(256), 0, s, a, w);
+                     dim3((unsigned)(w.mp / 64), (unsigned)(w.np / 64), batch), dim3(256), 0, s, a, w);
   for (int k = 0, from = 0; k < a.steps; ++k, from = 1 - from) {
     launch_product<kGram, BF16, PLANES>(a, w, from, s);
     launch_product<kSquare, BF16, PLANES>(a, w, from, s);
