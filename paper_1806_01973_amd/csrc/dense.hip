@@ -80,12 +80,6 @@ struct Piece {
   int64_t slot = 0;        // pieces of groups that have several, before this group
 };
 
-__device__ __forceinline__ int xcd_tile(int b, int nt) {
-  const int per = nt / 8, rem = nt % 8;
-  const int xcd = b % 8, slot = b / 8;
-  return xcd < rem ? xcd * (per + 1) + slot : rem * (per + 1) + (xcd - rem) * per + slot;
-}
-
 struct Groups {
   const int64_t* offsets;
   int G;

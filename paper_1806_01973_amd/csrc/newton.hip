@@ -168,11 +168,14 @@ enum NewtonProduct { kGram = 0, kSquare = 1, kApply = 2, kLast = 3 };
 // P[i][j] = sum_k L(i, k) R(j, k): Y^T Y, A A, or Y B (A and B are symmetric).
 template <class C, int KIND, bool BF16>
 __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch a, NewtonWork w,
-                                                                    int from) {
+                                                                    int from, int tiles) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[C::LDS_BYTES];
   constexpr int PLANES = C::MEM_PLANES;
   constexpr bool kSymmetric = KIND == kGram || KIND == kSquare;
-  const int64_t px = (int64_t)w.mp * w.np, pa = (int64_t)w.mp * w.mp, z = blockIdx.y;
+  const int64_t px = (int64_t)w.mp * w.np, pa = (int64_t)w.mp * w.mp;
+  // Neighbouring tiles, and whole matrices of a batch, on one XCD.
+  const int id = xcd_tile(blockIdx.x, gridDim.x), tile = id % tiles;
+  const int64_t z = id / tiles;
   const uint16_t* const Y = w.Y[from] + z * PLANES * px;
   uint16_t* const A = w.A + z * PLANES * pa;
   uint16_t* const B = w.B + z * PLANES * pa;
@@ -180,14 +183,14 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch
   if constexpr (kSymmetric) {
     // Tiles on and above the diagonal, row by row.
     const int T = w.mp / C::BM;
-    int left = blockIdx.x;
+    int left = tile;
     ti = 0;
     while (left >= T - ti) left -= T - ti++;
     tj = ti + left;
   } else {
     const int T = w.mp / C::BN;
-    ti = blockIdx.x / T;
-    tj = blockIdx.x % T;
+    ti = tile / T;
+    tj = tile % T;
   }
   const int i0 = ti * C::BM, j0 = tj * C::BN;
   Operand L, R;
@@ -517,8 +520,8 @@ inline bool small_tiles(const NewtonWork& w, int64_t batch, bool symmetric) {
 template <class C, int KIND, bool BF16>
 void launch_one(const NewtonLaunch& a, const NewtonWork& w, int from, hipStream_t s) {
   const int64_t tiles = tiles_of(w, 1, KIND == kGram || KIND == kSquare, C::BM);
-  hipLaunchKernelGGL((newton_kernel<C, KIND, BF16>), dim3((unsigned)tiles, (unsigned)a.batch),
-                     dim3(C::THREADS), 0, s, a, w, from);
+  hipLaunchKernelGGL((newton_kernel<C, KIND, BF16>), dim3((unsigned)(tiles * a.batch)),
+                     dim3(C::THREADS), 0, s, a, w, from, (int)tiles);
 }
 
 template <int KIND, bool BF16, int PLANES>

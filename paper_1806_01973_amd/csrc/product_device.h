@@ -76,6 +76,14 @@ struct ProductCfg {
   static_assert(BK == 32 || BK == 64 || BK == 128, "");
 };
 
+// Block b of nt to a tile: the hardware hands block b to XCD b % 8, this gives each
+// XCD a contiguous run of tiles, whose operands its L2 then shares.
+__device__ __forceinline__ int xcd_tile(int b, int nt) {
+  const int per = nt / 8, rem = nt % 8;
+  const int xcd = b % 8, slot = b / 8;
+  return xcd < rem ? xcd * (per + 1) + slot : rem * (per + 1) + (xcd - rem) * per + slot;
+}
+
 // Reads of any alignment: one wide load each on gfx950.
 template <typename T>
 __device__ __forceinline__ T load_any(const void* p) {
