@@ -523,7 +523,7 @@ typedef struct {
  * storage dtype. y may be the residual itself (same pointer and stride);
  * otherwise outputs overlap no input. Sums, bias, activation and residual in
  * fp32, each output rounded once. A row's bits follow from its own values, its
- * weight and the kernel that the sizes choose (few rows take another one). */
+ * weight and the kernel that the sizes and the rows' alignment choose. */
 int pinsage_dense_forward(const pinsage_dense_t* layer, const void* x, int64_t n, int64_t ldx,
                           const void* residual, int64_t ldr, void* u, int64_t ldu, void* y,
                           int64_t ldy, void* stream);

@@ -730,13 +730,14 @@ hipError_t dw_cfg(const DenseGradLaunch& a, hipStream_t s) {
   return hipGetLastError();
 }
 template <class CX, class CW>
-hipError_t grads_cfg(const DenseLaunch& x, const DenseGradLaunch& w, hipStream_t s) {
+bool grads_cfg(const DenseLaunch& x, const DenseGradLaunch& w, hipStream_t s, hipError_t* e) {
   const int64_t bw = dw_blocks<CW>(w), bx = rows_blocks<CX>(x);
-  if (bw + bx > 0x7FFFFFFFll) return hipErrorInvalidValue;
-  if (bw + bx > kGradsTogether) return hipErrorNotReady;  // launched apart
+  if (bw + bx > kGradsTogether) return false;
+  ProfileScope prof(kKDenseGrad, s);
   hipLaunchKernelGGL((dense_grads_kernel<CX, CW>), dim3((unsigned)(bw + bx)), dim3(CX::THREADS), 0, s,
                      x, w, (int)bw);
-  return hipGetLastError();
+  *e = hipGetLastError();
+  return true;
 }
 
 template <bool B_COL>
@@ -780,22 +781,24 @@ hipError_t dw_dtype(const DenseGradLaunch& a, hipStream_t s) {
   return shape == kSmall ? dw_cfg<typename T::Small>(a, s) : dw_cfg<typename T::Mid>(a, s);
 }
 
-// Both in one launch where both take ring tiles of four waves.
+// Both in one launch where both take ring tiles of four waves and are few; false: apart.
 template <bool BF16>
 bool grads_dtype(const DenseLaunch& x, const DenseGradLaunch& w, hipStream_t s, hipError_t* e) {
   using X = Tiles<BF16, false, true>;
   using W = Tiles<BF16, true, true>;
   const Shape sx = rows_shape(x, BF16), sw = dw_shape(w.n, w.N, w.K, w.G, BF16);
   if (sx == kBig || sw == kBig || !rows_vectors<true>(x) || !dw_vectors(w)) return false;
-  if (sx == kSmall && sw == kSmall) *e = grads_cfg<typename X::RingSmall, typename W::RingSmall>(x, w, s);
-  else if (sx == kSmall) *e = grads_cfg<typename X::RingSmall, typename W::RingMid>(x, w, s);
-  else if (sw == kSmall) *e = grads_cfg<typename X::RingMid, typename W::RingSmall>(x, w, s);
-  else *e = grads_cfg<typename X::RingMid, typename W::RingMid>(x, w, s);
-  return true;
+  if (sx == kSmall && sw == kSmall)
+    return grads_cfg<typename X::RingSmall, typename W::RingSmall>(x, w, s, e);
+  if (sx == kSmall) return grads_cfg<typename X::RingSmall, typename W::RingMid>(x, w, s, e);
+  if (sw == kSmall) return grads_cfg<typename X::RingMid, typename W::RingSmall>(x, w, s, e);
+  return grads_cfg<typename X::RingMid, typename W::RingMid>(x, w, s, e);
 }
 
+// Rows that a tile would not fill: up to 64, or 16 a group on average (the block of a
+// group that has most of them takes 64 at a time, so no more than 1,024 in all).
 bool few_rows_wanted(const DenseLaunch& a) {
-  return !a.b_col && a.M <= 16 * (int64_t)(a.offsets ? a.G : 4);
+  return !a.b_col && a.M <= (a.offsets ? std::min<int64_t>(16 * (int64_t)a.G, 1024) : 64);
 }
 
 }  // namespace
@@ -844,14 +847,9 @@ hipError_t launch_dense_dw(const DenseGradLaunch& a, hipStream_t s) {
 }
 
 hipError_t launch_dense_dx_dw(const DenseLaunch& x, const DenseGradLaunch& w, hipStream_t s) {
-  {
-    ProfileScope prof(kKDenseGrad, s);
-    hipError_t e = hipSuccess;
-    if ((w.bf16 ? grads_dtype<true>(x, w, s, &e) : grads_dtype<false>(x, w, s, &e)) &&
-        e != hipErrorNotReady)
-      return e;
-  }
-  const hipError_t e = launch_dense_rows(x, s);
+  hipError_t e = hipSuccess;
+  if (w.bf16 ? grads_dtype<true>(x, w, s, &e) : grads_dtype<false>(x, w, s, &e)) return e;
+  e = launch_dense_rows(x, s);
   return e != hipSuccess ? e : launch_dense_dw(w, s);
 }
 

@@ -334,6 +334,20 @@ def test_offsets_out_of_order_touch_nothing_outside():
         assert (guard[0] == 7).all() and (guard[201] == 7).all()
 
 
+def test_overlapping_groups_keep_to_the_workspace():
+    """Offsets that give every other group all rows count far more partial sums than the
+    workspace holds; the bytes after it stay."""
+    n, groups = 6000, 40
+    x, W, b, _, _ = make(n, 64, 48, "bf16", groups, [0] * groups)
+    off = torch.tensor([0, n] * (groups // 2) + [n], dtype=torch.int64).cuda()
+    dy = torch.ones(n, 48, dtype=torch.bfloat16, device="cuda")
+    need = ps().dense_backward_workspace_size(W.cuda(), n, "none", off)
+    whole = torch.full((need + 4096,), 77, dtype=torch.uint8, device="cuda")
+    ps().dense_backward(dy, x.cuda(), W.cuda(), offsets=off, workspace=whole[:need])
+    torch.cuda.synchronize()
+    assert (whole[need:] == 77).all()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_same_bits_again_and_on_another_stream(dtype):
     sizes = [700, 0, 1300, 90]
@@ -377,6 +391,38 @@ def test_captured_in_a_graph():
         assert torch.equal(y, want_y) and torch.equal(u, want_u)
         for p, q in zip(grads, want):
             assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("dtype,d_in", [("bf16", 2048), ("bf16", 2047), ("f32", 2048)])
+def test_rows_past_32_bits_of_elements(dtype, d_in):
+    """1.1M rows of 2,048: element offsets pass 2^31 (and bytes 2^32). Only the last rows
+    are not zero, so the sums are theirs."""
+    n, d_out, last = 1_100_000, 24, 300
+    _, W, b, _, _ = make(1, d_in, d_out, dtype, seed=13)
+    tail, _, _, dy, _ = make(last, d_in, d_out, dtype, seed=14)
+    x = torch.zeros(n, d_in, dtype=DT[dtype], device="cuda")
+    x[-last:] = tail.cuda()
+    y, u = ps().dense_forward(x, W.cuda(), b.cuda(), "silu", want_preact=True)
+    check_forward(tail, W, b, None, None, "silu", dtype, y[-last:], u[-last:])
+    assert (u[:-last] == b.cuda().to(DT[dtype])).all()
+    g = torch.zeros(n, d_out, dtype=DT[dtype], device="cuda")
+    g[-last:] = dy.cuda()
+    dx, dW, db = ps().dense_backward(g, x, W.cuda(), u, "silu")
+    assert not dx[:-last].any()
+    check_backward(tail, W, u[-last:].cpu(), dy, None, "silu", dtype, dx[-last:], dW, db)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sizes", [[500] + [0] * 63, [0] * 63 + [500], [3000] + [1] * 40,
+                                   [2100, 0, 0, 4000, 7, 1900]])
+def test_groups_that_hold_nearly_all_rows(sizes, dtype):
+    n = sum(sizes)
+    x, W, b, dy, off = make(n, 72, 56, dtype, len(sizes), sizes, seed=15)
+    y, u = ps().dense_forward(x.cuda(), W.cuda(), b.cuda(), "gelu", offsets=off.cuda(),
+                              want_preact=True)
+    check_forward(x, W, b, None, off, "gelu", dtype, y, u)
+    got = ps().dense_backward(dy.cuda(), x.cuda(), W.cuda(), u, "gelu", offsets=off.cuda())
+    check_backward(x, W, u.cpu(), dy, off, "gelu", dtype, *got)
 
 
 def test_refusals():
