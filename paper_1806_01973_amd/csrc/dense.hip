@@ -7,10 +7,10 @@
 //
 // The three products run on the same tile cores (ring_device.h where rows are whole
 // 16-byte vectors, else product_device.h): the forward's operands are both
-// k-contiguous, dx reads W by columns, dW reads dz and x by columns. dz is formed once, in the storage dtype (the products then read
-// 16-bit values; bf16 rounds it to 2^-9, which adds in quadrature to the same
-// rounding of dx and dW), by the kernel that also sums db, in fp32, from the
-// values before that rounding.
+// k-contiguous, dx reads W by columns, dW reads dz and x by columns. dz is formed
+// once, in the storage dtype (the products then read 16-bit values; bf16 rounds it
+// to 2^-9, which adds in quadrature to the same rounding of dx and dW), by the
+// kernel that also sums db, in fp32, from the values before that rounding.
 #include <algorithm>
 
 #include "kernels.h"
@@ -492,7 +492,7 @@ __global__ __launch_bounds__(256) void dense_dz_kernel(DenseGradLaunch a, int la
 // dW[g][n][k] = sum over the group's rows of dz[r][n] x[r][k]. Where the tiles of
 // dW alone leave CUs idle, a group's rows are cut into pieces of a.piece rows; a
 // group of several leaves fp32 partial sums in the workspace, which
-// dense_dw_join_kernel adds in order.
+// dense_join_kernel adds in order.
 template <class C>
 __device__ __forceinline__ void dw_block(const DenseGradLaunch& a, int block, int blocks,
                                          unsigned char* smem) {
@@ -551,7 +551,9 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void dense_dw_kernel(DenseGradL
 }
 
 // dx and dW in one launch, dW's blocks first: for few rows a launch costs as much as
-// either (about 5 us). With many blocks the two only take cache from each other
+// either (about 5 us). A whole backward pass, together against apart: 1,000 rows of
+// 256 -> 256 20.0 and 22.2 us (bf16), 20.1 and 27.8 (fp32); 4,596 of 512 -> 512 31.9
+// and 35.5, 61.5 and 67.9. With many blocks the two only take cache from each other
 // (60,000 x 1,024 -> 512 in 64 equal groups 220 us, apart 108 + 80).
 constexpr int64_t kGradsTogether = 1024;
 template <class CX, class CW>
@@ -690,11 +692,20 @@ constexpr int side(Shape s) { return s == kSmall ? 64 : (s == kMid ? 128 : 256);
 
 inline int64_t tiles_of(int64_t m, int64_t n, int b) { return ((m + b - 1) / b) * ((n + b - 1) / b); }
 
+// The larger the tile, the fewer bytes a product passes through LDS; the smaller, the
+// sooner the chip is full. Each limit with the forward's time on both sides, in us:
+//   bf16 64, 128:  512 tiles of 64: 8.6, 8.7 (1,024 -> 512); 1,024 tiles: 12.8, 10.9.
+//   bf16 128, 256: 128 tiles of 256: 16.4, 21.5; 256 tiles: 29.1, 25.1 (512 -> 512),
+//     44.6, 38.5 (1,024 -> 2,048). Up to 128 columns half of a 256-wide tile is empty:
+//     26.9, 39.0 (65,536 rows of 1,024 -> 128).
+//   bf16 groups, 1,024 -> 512: equal groups of 3,750 rows 83, 72; of 937 rows 85, 77,
+//     but uneven ones of 937 rows on average, with pre-activations, 133, 140.
+//   fp32 64, 128:  128 tiles of 128: 23.5, 31.9 (512 -> 512); 256 tiles: 39.5, 36.7.
 inline Shape rows_shape(const DenseLaunch& a, bool bf16) {
   const int64_t m = a.M, n = a.N;
-  if (!bf16) return tiles_of(m, n, 128) < 512 ? kSmall : kMid;
+  if (!bf16) return tiles_of(m, n, 128) < 256 ? kSmall : kMid;
   if (tiles_of(m, n, 64) <= 512) return kSmall;
-  if (a.offsets && m < 4096 * (int64_t)a.G) return kMid;
+  if (n <= 128 || (a.offsets && m < 2048 * (int64_t)a.G)) return kMid;
   return tiles_of(m, n, 256) < 256 ? kMid : kBig;
 }
 
@@ -760,11 +771,17 @@ hipError_t rows_dtype(const DenseLaunch& a, hipStream_t s) {
   return shape == kSmall ? rows_cfg<typename T::Small>(a, s) : rows_cfg<typename T::Mid>(a, s);
 }
 
-// Tiles of dW: 256 x 256 where eight pieces of them fill the chip (the partial sums of
-// more cost what the tile gains), 128 x 128 where pieces of 512 rows or more do.
+// Tiles of dW. 256 x 256 (bf16) where there are 8 of them or more and one round of
+// blocks takes 1,536 rows each or more: with fewer of either, the partial sums cost
+// what the tile gains. Times of dz, dW and the sums' join in us, by 128 and by 256:
+// 300,000 rows of 1,024 -> 2,048 1,962, 1,768; 60,000 of 1,024 -> 512 126, 122, in 64
+// groups 150, 124, in uneven ones 150, 145; 4,096 of 2,048 -> 2,048 (1,024 rows a
+// block) 66, 72; 200,000 of 512 -> 256 in 32 groups (2 tiles) 160, 161. 128 x 128
+// where pieces of 512 rows fill the chip; by 64 and by 128: 60,000 of 1,024 -> 512
+// in fp32 561, 434; 20,000 of 256 -> 256 25, 28 and 44, 48.
 inline Shape dw_shape(int64_t n, int N, int K, int G, bool bf16) {
-  const int64_t groups = G ? G : 1;
-  if (bf16 && n >= 4096 * groups && tiles_of(N, K, 256) * groups >= 32 && N > 128 && K > 128)
+  const int64_t tiles = tiles_of(N, K, 256);
+  if (bf16 && tiles >= 8 && n >= 512 * (int64_t)G && n * tiles >= 1536 * 256 && N > 128 && K > 128)
     return kBig;
   return tiles_of(N, K, 128) * (n / 512) >= 256 && N > 64 && K > 64 ? kMid : kSmall;
 }
@@ -795,10 +812,20 @@ bool grads_dtype(const DenseLaunch& x, const DenseGradLaunch& w, hipStream_t s, 
   return grads_cfg<typename X::RingMid, typename W::RingMid>(x, w, s, e);
 }
 
-// Rows that a tile would not fill: up to 64, or 16 a group on average (the block of a
-// group that has most of them takes 64 at a time, so no more than 1,024 in all).
+// Few rows: the weight goes through registers once, without LDS tiles. Times in us, by
+// this kernel and by tiles of 64. fp32, whose tiles split each weight first: up to 128
+// rows (512 -> 512 1 row 6.1, 13.2, 128 rows 12.2, 14.4, 256 rows 22.9, 14.5), or 16
+// a group on average (64 groups, 1,024 rows 20.1, 22.3, 2,048 rows 32.4, 23.2). bf16:
+// up to 32 rows (2,048 -> 4,096 8 rows 6.1, 9.7, 64 rows 11.6, 9.9), or 16 a group
+// in one round of blocks (8 groups, 1,024 -> 1,024, 128 rows 6.5, 7.1; 16 groups,
+// 2,048 -> 1,024, two rounds, 16.4, 12.5). A group that has most of the rows takes
+// them 64 at a time, hence the limits on the sum.
 bool few_rows_wanted(const DenseLaunch& a) {
-  return !a.b_col && a.M <= (a.offsets ? std::min<int64_t>(16 * (int64_t)a.G, 1024) : 64);
+  if (a.b_col) return false;
+  if (!a.offsets) return a.M <= (a.bf16 ? 32 : 128);
+  const int64_t blocks = (a.N + 15) / 16 * (a.G + 1), per_group = 16 * (int64_t)a.G;
+  return a.bf16 ? blocks <= 1024 && a.M <= std::min<int64_t>(per_group, 256)
+                : a.M <= std::min<int64_t>(per_group, 1024);
 }
 
 }  // namespace
@@ -817,13 +844,13 @@ hipError_t launch_dense_rows(const DenseLaunch& a, hipStream_t s) {
 }
 
 // Rows per piece of dW's sums: pieces that give every CU one round of blocks (one
-// block of 256 x 256, two of the others), two rounds with groups, whose sizes are
-// uneven; of 256 rows at least.
+// block of 256 x 256, two of the others), of 256 rows at least. More and smaller ones
+// even out uneven groups but cost partial sums: 60,000 rows of 1,024 -> 512 in 64
+// uneven groups 145 us, with pieces half as long 194.
 int64_t dense_dw_piece(int64_t n, int N, int K, int G, bool bf16) {
   const Shape shape = dw_shape(n, N, K, G, bf16);
   const int64_t tiles = tiles_of(N, K, side(shape));
-  const int64_t blocks = (shape == kBig ? 256 : 512) * (G > 1 ? 2 : 1);
-  const int64_t want = (blocks + tiles - 1) / tiles;
+  const int64_t want = ((shape == kBig ? 256 : 512) + tiles - 1) / tiles;
   const int64_t rows = ((n + want - 1) / want + 63) / 64 * 64;
   return rows < 256 ? 256 : rows;
 }

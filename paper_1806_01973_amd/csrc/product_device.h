@@ -23,7 +23,7 @@
 //           the leading one. Left out is at most 2^-25 of a product, as fp32's own
 //           rounding. Infinities and NaN, and values that round to a bf16
 //           infinity, make an element that is not finite; the caller takes such
-//           elements from product_dot.
+//           elements from redo_not_finite.
 // Sums run in fp32, chunks in order, so an element's bits follow from its row,
 // its column and the k range alone, whatever tile it lies in.
 #pragma once
