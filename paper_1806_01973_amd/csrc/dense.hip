@@ -672,8 +672,8 @@ template <bool BF16, bool A_COL, bool B_COL>
 struct Tiles;
 template <bool A_COL, bool B_COL>
 struct Tiles<true, A_COL, B_COL> {
-  using RingBig = RingCfg<kBf16, 256, 256, 64, 2, 4, A_COL, B_COL, 2>;
-  using RingMid = RingCfg<kBf16, 128, 128, 64, 2, 2, A_COL, B_COL, 2>;
+  using RingBig = RingCfg<kBf16, 256, 256, 64, 2, 4, A_COL, B_COL, 2, 1, 1>;
+  using RingMid = RingCfg<kBf16, 128, 128, 64, 2, 2, A_COL, B_COL, 2, 1, 1>;
   using RingSmall = RingCfg<kBf16, 64, 64, 64, 2, 2, A_COL, B_COL, 4>;
   using Mid = ProductCfg<kBf16, 128, 128, 64, 2, 2, A_COL, B_COL, 2>;
   using Small = ProductCfg<kBf16, 64, 64, 128, 2, 2, A_COL, B_COL, 2>;

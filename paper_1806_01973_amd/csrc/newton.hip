@@ -536,7 +536,7 @@ void launch_product(const NewtonLaunch& a, const NewtonWork& w, int from, hipStr
     else if (tiles_of(w, a.batch, kSymmetric, 128) <= 256)
       launch_one<RingCfg<kF16, 128, 128, 64, 2, 2, kCol, kCol, 4>, KIND, BF16>(a, w, from, s);
     else
-      launch_one<RingCfg<kF16, 128, 128, 64, 2, 2, kCol, kCol, 2>, KIND, BF16>(a, w, from, s);
+      launch_one<RingCfg<kF16, 128, 128, 64, 2, 2, kCol, kCol, 2, 1, 1>, KIND, BF16>(a, w, from, s);
   } else {
     if (small && tiles_of(w, a.batch, kSymmetric, 64) <= 256)
       launch_one<RingCfg<kF16x2, 64, 64, 64, 2, 2, kCol, kCol, 4>, KIND, BF16>(a, w, from, s);

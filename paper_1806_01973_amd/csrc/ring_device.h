@@ -34,9 +34,10 @@ namespace pinsage {
 __device__ __attribute__((aligned(16))) const uint32_t g_ring_zero[4] = {0, 0, 0, 0};
 
 template <int MODE_, int BM_, int BN_, int BK_, int WAVES_M_, int WAVES_N_, bool A_COL_,
-          bool B_COL_, int STAGES_, int WPE_ = 1>
+          bool B_COL_, int STAGES_, int WPE_ = 1, int AHEAD_ = 0>
 struct RingCfg {
   static constexpr int MODE = MODE_, BM = BM_, BN = BN_, BK = BK_, STAGES = STAGES_, WPE = WPE_;
+  static constexpr int AHEAD = AHEAD_;  // stages that A has beyond STAGES
   static constexpr int WAVES_M = WAVES_M_, WAVES_N = WAVES_N_;
   static constexpr bool A_COL = A_COL_, B_COL = B_COL_;
   static constexpr int NWAVES = WAVES_M * WAVES_N, THREADS = 64 * NWAVES;
@@ -44,16 +45,16 @@ struct RingCfg {
   static constexpr int ESZ = MODE == kF32 ? 4 : 2, MEM_PLANES = MODE == kF16x2 ? 2 : 1;
   static constexpr int PARTS = MODE == kF32 ? 3 : MEM_PLANES;  // of a fragment
   static constexpr int A_PLANE = BM * BK * ESZ, B_PLANE = BN * BK * ESZ;
-  static constexpr int BUF_BYTES = (A_PLANE + B_PLANE) * MEM_PLANES;
+  static constexpr int A_BYTES = A_PLANE * MEM_PLANES, B_BYTES = B_PLANE * MEM_PLANES;
   static constexpr int STEPS = BK / 16;  // k steps of a chunk
   // One DMA instruction of a wave fills a group of 1 KB.
   static constexpr int A_GROUPS = A_PLANE / 1024, B_GROUPS = B_PLANE / 1024;  // per plane
   static constexpr int DA = A_GROUPS * MEM_PLANES / NWAVES;  // of a wave, per chunk
   static constexpr int DB = B_GROUPS * MEM_PLANES / NWAVES;
-  static constexpr int PENDING = (STAGES - 2) * (DA + DB);
+  static constexpr int PENDING = (STAGES - 2) * (DA + DB) + AHEAD * DA;
   static constexpr int STAGE_LD = WN + 4;
   static constexpr int STAGE_BYTES = 32 * STAGE_LD * 4;
-  static constexpr int RING = STAGES * BUF_BYTES;
+  static constexpr int RING = (STAGES + AHEAD) * A_BYTES + STAGES * B_BYTES;
   static constexpr int LDS_BYTES = RING > NWAVES * STAGE_BYTES ? RING : NWAVES * STAGE_BYTES;
   static_assert(A_GROUPS * MEM_PLANES % NWAVES == 0 && B_GROUPS * MEM_PLANES % NWAVES == 0 &&
                     A_GROUPS % DA == 0 && B_GROUPS % DB == 0,
@@ -97,6 +98,15 @@ __device__ __forceinline__ const unsigned char* ring_uniform(const unsigned char
   return reinterpret_cast<const unsigned char*>(((uint64_t)hi << 32) | lo);
 }
 
+// f(integral_constant) for FROM .. TO - 1.
+template <int FROM, int TO, class F>
+__device__ __forceinline__ void unroll(F&& f) {
+  if constexpr (FROM < TO) {
+    f(std::integral_constant<int, FROM>{});
+    unroll<FROM + 1, TO>(f);
+  }
+}
+
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
@@ -106,6 +116,7 @@ template <class C>
 __device__ __forceinline__ void ring_tile(const Operand& A, const Operand& B, int64_t k0,
                                           int64_t k1, unsigned char* smem, TileSums<C>& sums) {
   constexpr int BK = C::BK, ESZ = C::ESZ, VE = 16 / ESZ, STAGES = C::STAGES;
+  constexpr int STAGES_A = STAGES + C::AHEAD;
   constexpr int PARTS = C::PARTS, PLANES = C::MEM_PLANES, SLOTS = BK / VE;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -158,32 +169,39 @@ __device__ __forceinline__ void ring_tile(const Operand& A, const Operand& B, in
   base_b = ring_uniform(base_b + (C::B_COL ? k0 * B.ld : k0) * ESZ);
   const int whole = __builtin_amdgcn_readfirstlane((int)((k1 - k0) / BK));  // chunks inside k
   const int rest = (int)((k1 - k0) % BK);
-  auto issue = [&](int c) __attribute__((always_inline)) {
-    const uint32_t dst = smem_base + (uint32_t)((c % STAGES) * C::BUF_BYTES);
-    const uint32_t dst_a = dst + first_a * 1024;
-    const uint32_t dst_b = dst + PLANES * C::A_PLANE + first_b * 1024;
-    if (c < whole) {
-#pragma unroll
-      for (int d = 0; d < DA; ++d)
-        ring_dma(base_a, off[d], __builtin_amdgcn_readfirstlane(dst_a + d * 1024));
-#pragma unroll
-      for (int d = 0; d < DB; ++d)
-        ring_dma(base_b, off[DA + d], __builtin_amdgcn_readfirstlane(dst_b + d * 1024));
-      base_a += step_a;
-      base_b += step_b;
+  // DMA d of a turn: B's of chunk `turn` and A's of chunk turn + AHEAD, in this order.
+  auto issue_one = [&](int turn, auto dma, auto inside) __attribute__((always_inline)) {
+    constexpr int d = decltype(dma)::value;
+    constexpr bool kOfA = d >= DB;
+    constexpr int at = kOfA ? d - DB : DA + d;  // in off and kk
+    const int c = kOfA ? turn + C::AHEAD : turn;
+    const uint32_t dst = __builtin_amdgcn_readfirstlane(
+        smem_base + (kOfA ? (uint32_t)(c % STAGES_A) * C::A_BYTES + (first_a + d - DB) * 1024
+                          : STAGES_A * C::A_BYTES + (uint32_t)(c % STAGES) * C::B_BYTES +
+                                (first_b + d) * 1024));
+    const unsigned char*& base = kOfA ? base_a : base_b;
+    if (decltype(inside)::value || c < whole) {
+      ring_dma(base, off[at], dst);
+      if constexpr (d == DB - 1) base_b += step_b;
+      if constexpr (d == DA + DB - 1) base_a += step_a;
     } else {
       // The last part of k, or beyond it: groups of zeros keep the count of loads in
       // flight the same.
-      const int left = c == whole ? rest : 0;
       const unsigned char* const zero = reinterpret_cast<const unsigned char*>(g_ring_zero);
-#pragma unroll
-      for (int d = 0; d < DA; ++d)
-        ring_dma_at(kk[d] < left ? base_a + off[d] : zero,
-                    __builtin_amdgcn_readfirstlane(dst_a + d * 1024));
-#pragma unroll
-      for (int d = 0; d < DB; ++d)
-        ring_dma_at(kk[DA + d] < left ? base_b + off[DA + d] : zero,
-                    __builtin_amdgcn_readfirstlane(dst_b + d * 1024));
+      ring_dma_at(kk[at] < (c == whole ? rest : 0) ? base + off[at] : zero, dst);
+    }
+  };
+  auto issue = [&](int turn, auto from, auto to) __attribute__((always_inline)) {
+    constexpr int d0 = decltype(from)::value, d1 = decltype(to)::value;
+    if constexpr (d0 < d1) {
+      if (turn + C::AHEAD < whole)
+        unroll<d0, d1>([&](auto d) __attribute__((always_inline)) {
+          issue_one(turn, d, std::true_type{});
+        });
+      else
+        unroll<d0, d1>([&](auto d) __attribute__((always_inline)) {
+          issue_one(turn, d, std::false_type{});
+        });
     }
   };
 
@@ -225,44 +243,33 @@ __device__ __forceinline__ void ring_tile(const Operand& A, const Operand& B, in
       }
     }
   };
-  // Step ks of chunk c.
+  // Fragment q of step ks of chunk c, of A's TM and B's TN.
+  auto read_one = [&](int c, int ks, Frags& f, auto frag) __attribute__((always_inline)) {
+    constexpr int q = decltype(frag)::value;
+    constexpr bool kOfA = q < C::TM, COL = kOfA ? C::A_COL : C::B_COL;
+    constexpr int width = kOfA ? C::BM : C::BN;
+    const unsigned char* const tile = kOfA ? smem + (c % STAGES_A) * C::A_BYTES
+                                           : smem + STAGES_A * C::A_BYTES + (c % STAGES) * C::B_BYTES;
+    const int m = kOfA ? wm * C::WM + 32 * q : wn * C::WN + 32 * (q - C::TM);
+    u32x4(&to)[PARTS] = kOfA ? f.a[kOfA ? q : 0] : f.b[kOfA ? 0 : q - C::TM];
+    unroll<0, PLANES>([&](auto plane) __attribute__((always_inline)) {
+      constexpr int p = decltype(plane)::value;
+      const unsigned char* const from = tile + p * (kOfA ? C::A_PLANE : C::B_PLANE);
+      u32x4(&out)[PARTS] = to;
+      if constexpr (PLANES == 1) {
+        if constexpr (COL) read_col(from, m, ks, width, out);
+        else read_row(from, m + frag_row, ks, out);
+      } else {
+        u32x4 x[PARTS];
+        if constexpr (COL) read_col(from, m, ks, width, x);
+        else read_row(from, m + frag_row, ks, x);
+        out[p] = x[0];
+      }
+    });
+  };
+  constexpr int FRAGS = C::TM + C::TN;
   auto read = [&](int c, int ks, Frags& f) __attribute__((always_inline)) {
-    const unsigned char* const a0 = smem + (c % STAGES) * C::BUF_BYTES;
-    const unsigned char* const b0 = a0 + PLANES * C::A_PLANE;
-#pragma unroll
-    for (int i = 0; i < C::TM; ++i) {
-      const int m = wm * C::WM + 32 * i;
-      if constexpr (PLANES == 2) {
-        u32x4 x[PARTS];
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          if constexpr (C::A_COL) read_col(a0 + p * C::A_PLANE, m, ks, C::BM, x);
-          else read_row(a0 + p * C::A_PLANE, m + frag_row, ks, x);
-          f.a[i][p] = x[0];
-        }
-      } else if constexpr (C::A_COL) {
-        read_col(a0, m, ks, C::BM, f.a[i]);
-      } else {
-        read_row(a0, m + frag_row, ks, f.a[i]);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < C::TN; ++j) {
-      const int n = wn * C::WN + 32 * j;
-      if constexpr (PLANES == 2) {
-        u32x4 x[PARTS];
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          if constexpr (C::B_COL) read_col(b0 + p * C::B_PLANE, n, ks, C::BN, x);
-          else read_row(b0 + p * C::B_PLANE, n + frag_row, ks, x);
-          f.b[j][p] = x[0];
-        }
-      } else if constexpr (C::B_COL) {
-        read_col(b0, n, ks, C::BN, f.b[j]);
-      } else {
-        read_row(b0, n + frag_row, ks, f.b[j]);
-      }
-    }
+    unroll<0, FRAGS>([&](auto q) __attribute__((always_inline)) { read_one(c, ks, f, q); });
   };
   auto split = [&](Frags& f) __attribute__((always_inline)) {
     if constexpr (ESZ == 4) {
@@ -281,61 +288,81 @@ __device__ __forceinline__ void ring_tile(const Operand& A, const Operand& B, in
       }
     }
   };
-  auto multiply = [&](const Frags& f) __attribute__((always_inline)) {
-    constexpr int PRODUCTS = PARTS * (PARTS + 1) / 2;
-#pragma unroll
-    for (int q = 0; q < PRODUCTS; ++q) {
-      constexpr int kB3[6] = {2, 0, 1, 1, 0, 0}, kA3[6] = {0, 2, 1, 0, 1, 0};
-      const int pb = kB3[6 - PRODUCTS + q], pa = kA3[6 - PRODUCTS + q];
-#pragma unroll
-      for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-        for (int j = 0; j < C::TN; ++j)
-          acc[i][j] = product_mfma<C::MODE>(f.b[j][pb], f.a[i][pa], acc[i][j]);
+  // A step: its products, the fragment reads of the next one (step ks of chunk c) and
+  // DMAs from .. to - 1 of a turn. With four MFMAs or more a step, reads and DMAs go one
+  // at a time among them, for in bursts they hold the wave, and its MFMAs, until the LDS
+  // and the address path, which all waves want at once, have taken them (bf16, 8,192
+  // cubed by 256 x 256: 1,005 us, the DMAs spread 979; with A a stage ahead 900, the
+  // reads spread too 878. By 64 x 64, one MFMA a step, it loses: 1,024 x 1,024 x 2,048
+  // 11.0 us, spread 15.0).
+  constexpr int PRODUCTS = PARTS * (PARTS + 1) / 2, ALL = PRODUCTS * C::TM * C::TN;
+  constexpr bool kSpread = ESZ == 2 && ALL >= 4;
+  auto work = [&](const Frags& cur, Frags& nxt, int c, int ks, int turn, auto from, auto to)
+      __attribute__((always_inline)) {
+    constexpr int D0 = decltype(from)::value, DMAS = decltype(to)::value - D0;
+    if constexpr (!kSpread) {
+      read(c, ks, nxt);
+      __builtin_amdgcn_sched_barrier(0);
+      issue(turn, from, to);
+      __builtin_amdgcn_sched_barrier(0);
+      split(nxt);
     }
-  };
-  // The products of a step, and the splitting of the next one's values among them.
-  auto work = [&](const Frags& cur, Frags& nxt) __attribute__((always_inline)) {
-    __builtin_amdgcn_sched_barrier(0);
-    split(nxt);
-    multiply(cur);
+    unroll<0, ALL>([&](auto at) __attribute__((always_inline)) {
+      constexpr int e = decltype(at)::value, q = e / (C::TM * C::TN), i = e / C::TN % C::TM,
+                    j = e % C::TN;
+      constexpr int kB3[6] = {2, 0, 1, 1, 0, 0}, kA3[6] = {0, 2, 1, 0, 1, 0};
+      constexpr int pb = kB3[6 - PRODUCTS + q], pa = kA3[6 - PRODUCTS + q];
+      acc[i][j] = product_mfma<C::MODE>(cur.b[j][pb], cur.a[i][pa], acc[i][j]);
+      if constexpr (kSpread) {
+        constexpr int r0 = (e * FRAGS + ALL - 1) / ALL, r1 = ((e + 1) * FRAGS + ALL - 1) / ALL;
+        constexpr int d0 = e * DMAS / ALL, d1 = (e + 1) * DMAS / ALL;
+        __builtin_amdgcn_sched_barrier(0);
+        unroll<r0, r1>([&](auto q) __attribute__((always_inline)) { read_one(c, ks, nxt, q); });
+        issue(turn, std::integral_constant<int, D0 + d0>{}, std::integral_constant<int, D0 + d1>{});
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    });
     if constexpr (ESZ == 4) {
-      constexpr int kMfma = 6 * C::TM * C::TN, kValu = 56 * (C::TM + C::TN);
+      // The splitting among the products.
+      constexpr int kValu = 56 * FRAGS;
 #pragma unroll
-      for (int q = 0; q < kMfma; ++q) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                            // MFMA
-        __builtin_amdgcn_sched_group_barrier(0x002, (kValu + kMfma - 1) / kMfma, 0);  // VALU
+      for (int q = 0; q < ALL; ++q) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                        // MFMA
+        __builtin_amdgcn_sched_group_barrier(0x002, (kValu + ALL - 1) / ALL, 0);  // VALU
       }
     }
     __builtin_amdgcn_sched_barrier(0);
   };
 
-  // Chunks 0 .. STAGES - 1 go out; a chunk is waited for (STAGES - 2 younger ones may
-  // stay in flight) and the barrier shows everybody's and frees the chunk before,
-  // whose stage takes chunk c + STAGES. The last step's MFMAs of a chunk follow that
-  // barrier, over the first fragment reads of the next.
+  // A chunk is waited for (STAGES - 2 younger ones may stay in flight) and the barrier
+  // shows everybody's and frees the chunk before, whose stage takes chunk c + STAGES:
+  // half of its DMAs go out in the last step of chunk c, whose MFMAs follow that
+  // barrier, over the first fragment reads of the next chunk, and half in the next step.
+  using None = std::integral_constant<int, 0>;
+  using Half = std::integral_constant<int, kSpread ? (DA + DB) / 2 : DA + DB>;
+  using Every = std::integral_constant<int, DA + DB>;
 #pragma unroll
-  for (int c = 0; c < STAGES - 1; ++c) issue(c);
+  for (int c = -C::AHEAD; c < 0; ++c) issue(c, std::integral_constant<int, DB>{}, Every{});
+#pragma unroll
+  for (int c = 0; c < STAGES - 1; ++c) issue(c, None{}, Every{});
   ring_wait<C::PENDING>();
   ring_barrier();
-  issue(STAGES - 1);
+  issue(STAGES - 1, None{}, Half{});
   Frags f[2];
   read(0, 0, f[0]);
   split(f[0]);
   auto chunk = [&](int c, auto parity) __attribute__((always_inline)) {
     constexpr int P = decltype(parity)::value;
-#pragma unroll
-    for (int s = 0; s + 1 < C::STEPS; ++s) {
-      read(c, s + 1, f[(P + s + 1) & 1]);
-      work(f[(P + s) & 1], f[(P + s + 1) & 1]);
-    }
+    unroll<0, C::STEPS - 1>([&](auto step) __attribute__((always_inline)) {
+      constexpr int s = decltype(step)::value;
+      Frags &cur = f[(P + s) & 1], &nxt = f[(P + s + 1) & 1];
+      if constexpr (s == 0) work(cur, nxt, c, s + 1, c + STAGES - 1, Half{}, Every{});
+      else work(cur, nxt, c, s + 1, 0, None{}, None{});
+    });
     ring_wait<C::PENDING>();
     ring_barrier();
-    Frags& nxt = f[(P + C::STEPS) & 1];
-    read(c + 1, 0, nxt);  // past the last chunk: zeros, unused
-    __builtin_amdgcn_sched_barrier(0);
-    issue(c + STAGES);
-    work(f[(P + C::STEPS - 1) & 1], nxt);
+    // Past the last chunk: zeros, unused.
+    work(f[(P + C::STEPS - 1) & 1], f[(P + C::STEPS) & 1], c + 1, 0, c + STAGES, None{}, Half{});
   };
   using Even = std::integral_constant<int, 0>;
   using Odd = std::integral_constant<int, 1>;
@@ -360,10 +387,10 @@ __device__ __forceinline__ void tile_sums(
     TileSums<ProductCfg<M, BM, BN, BK, WM, WN, AC, BC, NB, E>>& sums) {
   product_tile(A, B, k0, k1, smem, sums);
 }
-template <int M, int BM, int BN, int BK, int WM, int WN, bool AC, bool BC, int S, int E>
+template <int M, int BM, int BN, int BK, int WM, int WN, bool AC, bool BC, int S, int E, int H>
 __device__ __forceinline__ void tile_sums(
     const Operand& A, const Operand& B, int64_t k0, int64_t k1, unsigned char* smem,
-    TileSums<RingCfg<M, BM, BN, BK, WM, WN, AC, BC, S, E>>& sums) {
+    TileSums<RingCfg<M, BM, BN, BK, WM, WN, AC, BC, S, E, H>>& sums) {
   ring_tile(A, B, k0, k1, smem, sums);
 }
 
