@@ -675,6 +675,7 @@ struct Tiles<true, A_COL, B_COL> {
   using RingBig = RingCfg<kBf16, 256, 256, 64, 2, 4, A_COL, B_COL, 2, 1, 1>;
   using RingMid = RingCfg<kBf16, 128, 128, 64, 2, 2, A_COL, B_COL, 2, 1, 1>;
   using RingSmall = RingCfg<kBf16, 64, 64, 64, 2, 2, A_COL, B_COL, 4>;
+  using RingMany = RingCfg<kBf16, 64, 64, 64, 2, 2, A_COL, B_COL, 2>;
   using Mid = ProductCfg<kBf16, 128, 128, 64, 2, 2, A_COL, B_COL, 2>;
   using Small = ProductCfg<kBf16, 64, 64, 128, 2, 2, A_COL, B_COL, 2>;
 };
@@ -682,6 +683,7 @@ template <bool A_COL, bool B_COL>
 struct Tiles<false, A_COL, B_COL> {
   using RingMid = RingCfg<kF32, 128, 128, 16, 2, 2, A_COL, B_COL, 4, 2>;
   using RingSmall = RingCfg<kF32, 64, 64, 16, 2, 2, A_COL, B_COL, 4>;
+  using RingMany = RingSmall;
   using RingBig = RingMid;
   using Mid = ProductCfg<kF32, 128, 128, 32, 2, 2, A_COL, B_COL, 1>;
   using Small = ProductCfg<kF32, 64, 64, 64, 2, 2, A_COL, B_COL, 1>;
@@ -694,20 +696,26 @@ inline int64_t tiles_of(int64_t m, int64_t n, int b) { return ((m + b - 1) / b) 
 
 // The larger the tile, the fewer bytes a product passes through LDS; the smaller, the
 // sooner the chip is full. Each limit with the forward's time on both sides, in us:
-//   bf16 64, 128:  512 tiles of 64: 8.6, 8.7 (1,024 -> 512); 1,024 tiles: 12.8, 10.9.
+//   bf16 64, 128:  576 tiles of 64: 7.9, 10.5 (512 -> 512); 1,024 tiles: 10.9, 10.9;
+//     by the register core 752 tiles: 18.7, 14.6 (300 -> 500).
 //   bf16 128, 256: 128 tiles of 256: 16.4, 21.5; 256 tiles: 29.1, 25.1 (512 -> 512),
 //     44.6, 38.5 (1,024 -> 2,048). Up to 128 columns half of a 256-wide tile is empty:
 //     26.9, 39.0 (65,536 rows of 1,024 -> 128).
 //   bf16 groups, 1,024 -> 512: equal groups of 3,750 rows 83, 72; of 937 rows 85, 77,
 //     but uneven ones of 937 rows on average, with pre-activations, 133, 140.
 //   fp32 64, 128:  128 tiles of 128: 23.5, 31.9 (512 -> 512); 256 tiles: 39.5, 36.7.
-inline Shape rows_shape(const DenseLaunch& a, bool bf16) {
+inline Shape rows_shape(const DenseLaunch& a, bool bf16, bool ring) {
   const int64_t m = a.M, n = a.N;
   if (!bf16) return tiles_of(m, n, 128) < 256 ? kSmall : kMid;
-  if (tiles_of(m, n, 64) <= 512) return kSmall;
+  if (tiles_of(m, n, 64) <= (ring ? 768 : 512)) return kSmall;
   if (n <= 128 || (a.offsets && m < 2048 * (int64_t)a.G)) return kMid;
   return tiles_of(m, n, 256) < 256 ? kMid : kBig;
 }
+
+// Tiles of 64 in bf16 have four stages of 16 KB, which two blocks a CU hold; where
+// there are more blocks than that, two stages, so that they run together: 576 tiles of
+// depth 512 8.5 us with two, 11.4 with four; 256 tiles of depth 2,048 18.5 and 11.4.
+inline bool many(int64_t blocks) { return blocks > 512; }
 
 inline bool vectors(const void* p, int64_t ld, int64_t width, bool bf16) {
   const int64_t ve = bf16 ? 8 : 4;
@@ -762,9 +770,12 @@ bool dw_vectors(const DenseGradLaunch& a) {
 template <bool BF16, bool B_COL>
 hipError_t rows_dtype(const DenseLaunch& a, hipStream_t s) {
   using T = Tiles<BF16, false, B_COL>;
-  const Shape shape = rows_shape(a, BF16);
-  if (rows_vectors<B_COL>(a)) {
-    if (shape == kSmall) return rows_cfg<typename T::RingSmall>(a, s);
+  const bool ring = rows_vectors<B_COL>(a);
+  const Shape shape = rows_shape(a, BF16, ring);
+  if (ring) {
+    if (shape == kSmall)
+      return many(rows_blocks<typename T::RingSmall>(a)) ? rows_cfg<typename T::RingMany>(a, s)
+                                                         : rows_cfg<typename T::RingSmall>(a, s);
     if (shape == kMid) return rows_cfg<typename T::RingMid>(a, s);
     return rows_cfg<typename T::RingBig>(a, s);
   }
@@ -791,7 +802,9 @@ hipError_t dw_dtype(const DenseGradLaunch& a, hipStream_t s) {
   using T = Tiles<BF16, true, true>;
   const Shape shape = dw_shape(a.n, a.N, a.K, a.G, BF16);
   if (dw_vectors(a)) {
-    if (shape == kSmall) return dw_cfg<typename T::RingSmall>(a, s);
+    if (shape == kSmall)
+      return many(dw_blocks<typename T::RingSmall>(a)) ? dw_cfg<typename T::RingMany>(a, s)
+                                                       : dw_cfg<typename T::RingSmall>(a, s);
     if (shape == kMid) return dw_cfg<typename T::RingMid>(a, s);
     return dw_cfg<typename T::RingBig>(a, s);
   }
@@ -803,10 +816,14 @@ template <bool BF16>
 bool grads_dtype(const DenseLaunch& x, const DenseGradLaunch& w, hipStream_t s, hipError_t* e) {
   using X = Tiles<BF16, false, true>;
   using W = Tiles<BF16, true, true>;
-  const Shape sx = rows_shape(x, BF16), sw = dw_shape(w.n, w.N, w.K, w.G, BF16);
-  if (sx == kBig || sw == kBig || !rows_vectors<true>(x) || !dw_vectors(w)) return false;
-  if (sx == kSmall && sw == kSmall)
+  if (!rows_vectors<true>(x) || !dw_vectors(w)) return false;
+  const Shape sx = rows_shape(x, BF16, true), sw = dw_shape(w.n, w.N, w.K, w.G, BF16);
+  if (sx == kBig || sw == kBig) return false;
+  if (sx == kSmall && sw == kSmall) {
+    if (many(rows_blocks<typename X::RingSmall>(x) + dw_blocks<typename W::RingSmall>(w)))
+      return grads_cfg<typename X::RingMany, typename W::RingMany>(x, w, s, e);
     return grads_cfg<typename X::RingSmall, typename W::RingSmall>(x, w, s, e);
+  }
   if (sx == kSmall) return grads_cfg<typename X::RingSmall, typename W::RingMid>(x, w, s, e);
   if (sw == kSmall) return grads_cfg<typename X::RingMid, typename W::RingSmall>(x, w, s, e);
   return grads_cfg<typename X::RingMid, typename W::RingMid>(x, w, s, e);
