@@ -5,9 +5,8 @@
 // (ragged: group g holds rows offsets[g] .. offsets[g + 1] - 1, read on the
 // device; empty groups allowed).
 //
-// The three products run on the same tile cores (ring_device.h where rows are whole
-// 16-byte vectors, else product_device.h): the forward's operands are both
-// k-contiguous, dx reads W by columns, dW reads dz and x by columns. dz is formed
+// The three products run on the same tiles (ring_device.h): the forward's operands are
+// both k-contiguous, dx reads W by columns, dW reads dz and x by columns. dz is formed
 // once, in the storage dtype (the products then read 16-bit values; bf16 rounds it
 // to 2^-9, which adds in quadrature to the same rounding of dx and dW), by the
 // kernel that also sums db, in fp32, from the values before that rounding.
@@ -229,7 +228,7 @@ __device__ __forceinline__ void rows_block(const DenseLaunch& a, int block, int 
   TileSums<C> sums;
   const Operand A{Ap, a.lda, valid, 0};
   const Operand B{Bg + (C::B_COL ? (int64_t)n0 : n0 * a.ldb) * C::ESZ, a.ldb,
-                  a.N - n0 < C::BN ? a.N - n0 : C::BN, 0};
+                  a.N - n0 < C::BN ? a.N - n0 : C::BN, 0, n0};
   // The residual's tile is touched, a value per 128 bytes, so that it lies in L2 when the
   // epilogue reads it (60,000 x 1,024 -> 512 bf16: 24 us on top of 73 without).
   const unsigned char* const res =
@@ -522,7 +521,7 @@ __device__ __forceinline__ void dw_block(const DenseGradLaunch& a, int block, in
   const unsigned char* const X =
       static_cast<const unsigned char*>(a.x) + (r0 * a.ldx + k0) * C::ESZ;
   TileSums<C> sums;
-  tile_sums(Operand{Z, a.lddz, vn, 0}, Operand{X, a.ldx, vk, 0}, 0, rows, smem, sums);
+  tile_sums(Operand{Z, a.lddz, vn, 0, n0}, Operand{X, a.ldx, vk, 0, k0}, 0, rows, smem, sums);
   // Offsets that overlap could count more pieces than the workspace holds.
   if (p.pieces > 1 && p.slot + p.index >= dense_dw_parts(a.n, a.piece, a.offsets ? a.G : 0)) return;
   float* const part = p.pieces > 1 ? a.dw_parts + (p.slot + p.index) * (int64_t)a.N * a.K : nullptr;
@@ -666,8 +665,8 @@ __global__ __launch_bounds__(64 * kJoinWaves) void dense_join_kernel(DenseGradLa
 }
 
 // ---- tile shapes -----------------------------------------------------------------
-// Ring: rows of whole 16-byte vectors; else the register core, which has no
-// 256 x 256 tile.
+// Ring: rows of whole 16-byte vectors; else through registers, which 256 x 256 leaves
+// none of.
 template <bool BF16, bool A_COL, bool B_COL>
 struct Tiles;
 template <bool A_COL, bool B_COL>
@@ -676,8 +675,8 @@ struct Tiles<true, A_COL, B_COL> {
   using RingMid = RingCfg<kBf16, 128, 128, 64, 2, 2, A_COL, B_COL, 2, 1, 1>;
   using RingSmall = RingCfg<kBf16, 64, 64, 64, 2, 2, A_COL, B_COL, 4>;
   using RingMany = RingCfg<kBf16, 64, 64, 64, 2, 2, A_COL, B_COL, 2>;
-  using Mid = ProductCfg<kBf16, 128, 128, 64, 2, 2, A_COL, B_COL, 2>;
-  using Small = ProductCfg<kBf16, 64, 64, 128, 2, 2, A_COL, B_COL, 2>;
+  using Mid = RingCfg<kBf16, 128, 128, 64, 2, 2, A_COL, B_COL, 2, 1, 0, true>;
+  using Small = RingCfg<kBf16, 64, 64, 64, 2, 2, A_COL, B_COL, 2, 4, 0, true>;
 };
 template <bool A_COL, bool B_COL>
 struct Tiles<false, A_COL, B_COL> {
@@ -685,8 +684,8 @@ struct Tiles<false, A_COL, B_COL> {
   using RingSmall = RingCfg<kF32, 64, 64, 16, 2, 2, A_COL, B_COL, 4>;
   using RingMany = RingSmall;
   using RingBig = RingMid;
-  using Mid = ProductCfg<kF32, 128, 128, 32, 2, 2, A_COL, B_COL, 1>;
-  using Small = ProductCfg<kF32, 64, 64, 64, 2, 2, A_COL, B_COL, 1>;
+  using Mid = RingCfg<kF32, 128, 128, 16, 2, 2, A_COL, B_COL, 2, 2, 0, true>;
+  using Small = RingCfg<kF32, 64, 64, 32, 2, 2, A_COL, B_COL, 2, 3, 0, true>;
 };
 
 enum Shape { kSmall, kMid, kBig };
@@ -697,17 +696,17 @@ inline int64_t tiles_of(int64_t m, int64_t n, int b) { return ((m + b - 1) / b) 
 // The larger the tile, the fewer bytes a product passes through LDS; the smaller, the
 // sooner the chip is full. Each limit with the forward's time on both sides, in us:
 //   bf16 64, 128:  576 tiles of 64: 7.9, 10.5 (512 -> 512); 1,024 tiles: 10.9, 10.9;
-//     by the register core 752 tiles: 18.7, 14.6 (300 -> 500).
+//     through registers 752 tiles: 9.8, 12.2 (300 -> 500).
 //   bf16 128, 256: 128 tiles of 256: 16.4, 21.5; 256 tiles: 29.1, 25.1 (512 -> 512),
 //     44.6, 38.5 (1,024 -> 2,048). Up to 128 columns half of a 256-wide tile is empty:
 //     26.9, 39.0 (65,536 rows of 1,024 -> 128).
 //   bf16 groups, 1,024 -> 512: equal groups of 3,750 rows 83, 72; of 937 rows 85, 77,
 //     but uneven ones of 937 rows on average, with pre-activations, 133, 140.
 //   fp32 64, 128:  128 tiles of 128: 23.5, 31.9 (512 -> 512); 256 tiles: 39.5, 36.7.
-inline Shape rows_shape(const DenseLaunch& a, bool bf16, bool ring) {
+inline Shape rows_shape(const DenseLaunch& a, bool bf16) {
   const int64_t m = a.M, n = a.N;
   if (!bf16) return tiles_of(m, n, 128) < 256 ? kSmall : kMid;
-  if (tiles_of(m, n, 64) <= (ring ? 768 : 512)) return kSmall;
+  if (tiles_of(m, n, 64) <= 768) return kSmall;
   if (n <= 128 || (a.offsets && m < 2048 * (int64_t)a.G)) return kMid;
   return tiles_of(m, n, 256) < 256 ? kMid : kBig;
 }
@@ -771,7 +770,7 @@ template <bool BF16, bool B_COL>
 hipError_t rows_dtype(const DenseLaunch& a, hipStream_t s) {
   using T = Tiles<BF16, false, B_COL>;
   const bool ring = rows_vectors<B_COL>(a);
-  const Shape shape = rows_shape(a, BF16, ring);
+  const Shape shape = rows_shape(a, BF16);
   if (ring) {
     if (shape == kSmall)
       return many(rows_blocks<typename T::RingSmall>(a)) ? rows_cfg<typename T::RingMany>(a, s)
@@ -817,7 +816,7 @@ bool grads_dtype(const DenseLaunch& x, const DenseGradLaunch& w, hipStream_t s, 
   using X = Tiles<BF16, false, true>;
   using W = Tiles<BF16, true, true>;
   if (!rows_vectors<true>(x) || !dw_vectors(w)) return false;
-  const Shape sx = rows_shape(x, BF16, true), sw = dw_shape(w.n, w.N, w.K, w.G, BF16);
+  const Shape sx = rows_shape(x, BF16), sw = dw_shape(w.n, w.N, w.K, w.G, BF16);
   if (sx == kBig || sw == kBig) return false;
   if (sx == kSmall && sw == kSmall) {
     if (many(rows_blocks<typename X::RingSmall>(x) + dw_blocks<typename W::RingSmall>(w)))

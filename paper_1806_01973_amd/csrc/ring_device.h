@@ -1,11 +1,15 @@
-// The tile product of product_device.h for operands whose rows are whole 16-byte
-// vectors, fed by DMA.
+// One output tile of C[m][n] = sum_k A(m, k) B(n, k), its operands fed through a ring of
+// stages in LDS.
 //
-// Chunks of BK columns of k travel global -> LDS directly (no registers, no
-// VALU beside one scalar add per chunk) into a ring of STAGES stages, up to
-// STAGES chunks ahead of the MFMAs, with one barrier per chunk: the register
-// path has one chunk in flight, and where a CU holds one tile a chunk's MFMAs
-// (0.2 us at 128 x 128 x 64) are far shorter than a load's latency.
+// Chunks of BK columns of k travel global -> LDS by DMA (no registers, no VALU beside
+// one scalar add per chunk), up to STAGES chunks ahead of the MFMAs, with one barrier
+// per chunk: where a CU holds one tile a chunk's MFMAs (0.2 us at 128 x 128 x 64) are
+// far shorter than a load's latency. AHEAD gives A, the operand that comes from HBM
+// where B is a weight that L2 holds, a stage more than B: 8,192 cubed by 256 x 256
+// 979 us, with it 900; by 128 x 128 1,425 and 1,217.
+// DMAs take whole aligned 16-byte vectors. Operands whose rows are not (REGS) come
+// through registers, a chunk held there beside the two in LDS, with loads of any
+// alignment; a vector across the end of a row is the one that ends there, shifted.
 // A row operand lies in LDS as rows of BK values, 16-byte slot v of row r at
 // v ^ swizzle(r); a column operand as it lies in memory, BK rows of BM values. Of
 // 16-bit values its fragments come through the transposing LDS read (16 lanes read
@@ -23,6 +27,8 @@
 // larger wave tiles, gained 5% at most and are not here.
 // Where rows end inside a tile, lanes read the last row or vector again (the
 // results of those rows are never used); past the end of k they read zeros.
+// bf16, 300,000 x 1,024 -> 2,048 by 256 x 256 1,332 us (945 TFLOP/s), the epilogue with
+// it; 4,596 x 512 -> 512 by 64 x 64 7.9 us, 511 -> 511 (REGS) 11.9.
 #pragma once
 
 #include <type_traits>
@@ -34,11 +40,12 @@ namespace pinsage {
 __device__ __attribute__((aligned(16))) const uint32_t g_ring_zero[4] = {0, 0, 0, 0};
 
 template <int MODE_, int BM_, int BN_, int BK_, int WAVES_M_, int WAVES_N_, bool A_COL_,
-          bool B_COL_, int STAGES_, int WPE_ = 1, int AHEAD_ = 0>
+          bool B_COL_, int STAGES_, int WPE_ = 1, int AHEAD_ = 0, bool REGS_ = false>
 struct RingCfg {
   static constexpr int MODE = MODE_, BM = BM_, BN = BN_, BK = BK_, STAGES = STAGES_, WPE = WPE_;
   static constexpr int AHEAD = AHEAD_;  // stages that A has beyond STAGES
   static constexpr int WAVES_M = WAVES_M_, WAVES_N = WAVES_N_;
+  static constexpr bool REGS = REGS_;  // chunks go through registers: any alignment
   static constexpr bool A_COL = A_COL_, B_COL = B_COL_;
   static constexpr int NWAVES = WAVES_M * WAVES_N, THREADS = 64 * NWAVES;
   static constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, TM = WM / 32, TN = WN / 32;
@@ -60,6 +67,7 @@ struct RingCfg {
                     A_GROUPS % DA == 0 && B_GROUPS % DB == 0,
                 "every wave serves one plane of each operand");
   static_assert(STAGES >= 2 && PENDING <= 63 && LDS_BYTES <= 160 * 1024, "");
+  static_assert(!REGS || (MEM_PLANES == 1 && AHEAD == 0), "");
   static_assert(BK * ESZ == 64 || BK * ESZ == 128, "rows of 4 or 8 slots");
 };
 
@@ -110,10 +118,12 @@ __device__ __forceinline__ void unroll(F&& f) {
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// As product_tile; operands' `p` and `ld` multiples of 16 bytes, and so the
-// `valid` values of a column operand and the k1 - k0 of a row operand.
+// The tile's products over k in [k0, k1). All of the block's threads call it; smem
+// holds C::LDS_BYTES and is free again when it returns (after a barrier). Without
+// C::REGS, operands' `p` and `ld` are multiples of 16 bytes, and so are the `valid`
+// values of a column operand and the k1 - k0 of a row operand.
 template <class C>
-__device__ __forceinline__ void ring_tile(const Operand& A, const Operand& B, int64_t k0,
+__device__ __forceinline__ void tile_sums(const Operand& A, const Operand& B, int64_t k0,
                                           int64_t k1, unsigned char* smem, TileSums<C>& sums) {
   constexpr int BK = C::BK, ESZ = C::ESZ, VE = 16 / ESZ, STAGES = C::STAGES;
   constexpr int STAGES_A = STAGES + C::AHEAD;
@@ -147,7 +157,7 @@ __device__ __forceinline__ void ring_tile(const Operand& A, const Operand& B, in
     if constexpr (decltype(column)::value) {
       const int spr = width / VE, k = g * 64 / spr + lane / spr;
       int m = ((lane % spr) ^ (ESZ == 2 ? ring_col_swizzle(k) : 0)) * VE;
-      m = m < o.valid ? m : o.valid - VE;
+      if constexpr (!C::REGS) m = m < o.valid ? m : o.valid - VE;
       off[d] = ((uint32_t)k * (uint32_t)o.ld + (uint32_t)m) * ESZ;
       kk[d] = k;
     } else {
@@ -203,6 +213,63 @@ __device__ __forceinline__ void ring_tile(const Operand& A, const Operand& B, in
           issue_one(turn, d, std::false_type{});
         });
     }
+  };
+
+  // ---- the same through registers ---------------------------------------------------
+  // The vector's first m of a column operand: one for all of the lane's.
+  auto first_m = [&](int width) __attribute__((always_inline)) {
+    const int spr = width / VE;
+    return ((lane % spr) ^ (ESZ == 2 ? ring_col_swizzle(lane / spr) : 0)) * VE;
+  };
+  const int m_a = C::A_COL ? first_m(C::BM) : 0, m_b = C::B_COL ? first_m(C::BN) : 0;
+  // Whether the tile has no edge, and a vector of existing elements fits each operand's rows.
+  const bool inner = (!C::A_COL || A.valid >= C::BM) && (!C::B_COL || B.valid >= C::BN);
+  const bool room = (C::A_COL ? A.before + A.valid : k1 - k0) >= VE &&
+                    (C::B_COL ? B.before + B.valid : k1 - k0) >= VE;
+  auto fetch = [&](int c, u32x4(&v)[DA + DB]) __attribute__((always_inline)) {
+    if (c >= nchunks) return;
+    const int left = c < whole ? BK : rest;
+    // How many elements of a vector exist.
+    auto count = [&](auto dma) __attribute__((always_inline)) {
+      constexpr int d = decltype(dma)::value;
+      constexpr bool kOfA = d < DA;
+      const int have = (kOfA ? C::A_COL : C::B_COL)
+                           ? (kk[d] < left ? (kOfA ? A.valid - m_a : B.valid - m_b) : 0)
+                           : left - kk[d];
+      return have < 0 ? 0 : (have < VE ? have : VE);
+    };
+    if (c < whole && inner) {
+      unroll<0, DA + DB>([&](auto dma) __attribute__((always_inline)) {
+        constexpr int d = decltype(dma)::value;
+        v[d] = load_any<u32x4>((d < DA ? base_a : base_b) + off[d]);
+      });
+    } else if (room) {
+      // The vector that ends where the elements do, shifted.
+      unroll<0, DA + DB>([&](auto dma) __attribute__((always_inline)) {
+        constexpr int d = decltype(dma)::value;
+        const int have = count(dma);
+        const unsigned char* const p = (d < DA ? base_a : base_b) + off[d] - (VE - have) * ESZ;
+        const unsigned char* const zero = reinterpret_cast<const unsigned char*>(g_ring_zero);
+        v[d] = drop_first<ESZ>(load_any<u32x4>(have ? p : zero), VE - have);
+      });
+    } else {
+      unroll<0, DA + DB>([&](auto dma) __attribute__((always_inline)) {
+        constexpr int d = decltype(dma)::value;
+        v[d] = load_few<ESZ>((d < DA ? base_a : base_b) + off[d], count(dma));
+      });
+    }
+    base_a += step_a;
+    base_b += step_b;
+  };
+  auto store = [&](int c, const u32x4(&v)[DA + DB]) __attribute__((always_inline)) {
+    if (c >= nchunks) return;
+    unsigned char* const to_a = smem + (c % STAGES) * C::A_BYTES + first_a * 1024 + lane * 16;
+    unsigned char* const to_b =
+        smem + STAGES * C::A_BYTES + (c % STAGES) * C::B_BYTES + first_b * 1024 + lane * 16;
+    unroll<0, DA + DB>([&](auto dma) __attribute__((always_inline)) {
+      constexpr int d = decltype(dma)::value;
+      *reinterpret_cast<u32x4*>(d < DA ? to_a + d * 1024 : to_b + (d - DA) * 1024) = v[d];
+    });
   };
 
   // ---- fragments ------------------------------------------------------------------
@@ -341,13 +408,24 @@ __device__ __forceinline__ void ring_tile(const Operand& A, const Operand& B, in
   using None = std::integral_constant<int, 0>;
   using Half = std::integral_constant<int, kSpread ? (DA + DB) / 2 : DA + DB>;
   using Every = std::integral_constant<int, DA + DB>;
+  u32x4 held[DA + DB];  // REGS: chunk c + STAGES, until chunk c's stage is free
+  if constexpr (C::REGS) {
+    u32x4 first[STAGES][DA + DB];
 #pragma unroll
-  for (int c = -C::AHEAD; c < 0; ++c) issue(c, std::integral_constant<int, DB>{}, Every{});
+    for (int c = 0; c < STAGES; ++c) fetch(c, first[c]);
+    fetch(STAGES, held);
 #pragma unroll
-  for (int c = 0; c < STAGES - 1; ++c) issue(c, None{}, Every{});
-  ring_wait<C::PENDING>();
-  ring_barrier();
-  issue(STAGES - 1, None{}, Half{});
+    for (int c = 0; c < STAGES; ++c) store(c, first[c]);
+    ring_barrier();
+  } else {
+#pragma unroll
+    for (int c = -C::AHEAD; c < 0; ++c) issue(c, std::integral_constant<int, DB>{}, Every{});
+#pragma unroll
+    for (int c = 0; c < STAGES - 1; ++c) issue(c, None{}, Every{});
+    ring_wait<C::PENDING>();
+    ring_barrier();
+    issue(STAGES - 1, None{}, Half{});
+  }
   Frags f[2];
   read(0, 0, f[0]);
   split(f[0]);
@@ -356,42 +434,37 @@ __device__ __forceinline__ void ring_tile(const Operand& A, const Operand& B, in
     unroll<0, C::STEPS - 1>([&](auto step) __attribute__((always_inline)) {
       constexpr int s = decltype(step)::value;
       Frags &cur = f[(P + s) & 1], &nxt = f[(P + s + 1) & 1];
-      if constexpr (s == 0) work(cur, nxt, c, s + 1, c + STAGES - 1, Half{}, Every{});
+      if constexpr (s == 0 && !C::REGS) work(cur, nxt, c, s + 1, c + STAGES - 1, Half{}, Every{});
       else work(cur, nxt, c, s + 1, 0, None{}, None{});
     });
-    ring_wait<C::PENDING>();
+    if constexpr (!C::REGS) ring_wait<C::PENDING>();
     ring_barrier();
-    // Past the last chunk: zeros, unused.
-    work(f[(P + C::STEPS - 1) & 1], f[(P + C::STEPS) & 1], c + 1, 0, c + STAGES, None{}, Half{});
+    // Past the last chunk what is read is not used.
+    Frags &cur = f[(P + C::STEPS - 1) & 1], &nxt = f[(P + C::STEPS) & 1];
+    if constexpr (C::REGS) {
+      work(cur, nxt, c + 1, 0, 0, None{}, None{});
+      store(c + STAGES, held);
+      fetch(c + STAGES + 1, held);
+    } else {
+      work(cur, nxt, c + 1, 0, c + STAGES, None{}, Half{});
+    }
   };
   using Even = std::integral_constant<int, 0>;
   using Odd = std::integral_constant<int, 1>;
   int c = 0;
   if constexpr (C::STEPS % 2) {
+#pragma unroll 1
     for (; c + 1 < nchunks; c += 2) {
       chunk(c, Even{});
       chunk(c + 1, Odd{});
     }
     if (c < nchunks) chunk(c, Even{});
   } else {
+#pragma unroll 1
     for (; c < nchunks; ++c) chunk(c, Even{});
   }
-  ring_wait<0>();
+  if constexpr (!C::REGS) ring_wait<0>();
   __syncthreads();
-}
-
-// The tile product a configuration stands for.
-template <int M, int BM, int BN, int BK, int WM, int WN, bool AC, bool BC, int NB, int E>
-__device__ __forceinline__ void tile_sums(
-    const Operand& A, const Operand& B, int64_t k0, int64_t k1, unsigned char* smem,
-    TileSums<ProductCfg<M, BM, BN, BK, WM, WN, AC, BC, NB, E>>& sums) {
-  product_tile(A, B, k0, k1, smem, sums);
-}
-template <int M, int BM, int BN, int BK, int WM, int WN, bool AC, bool BC, int S, int E, int H>
-__device__ __forceinline__ void tile_sums(
-    const Operand& A, const Operand& B, int64_t k0, int64_t k1, unsigned char* smem,
-    TileSums<RingCfg<M, BM, BN, BK, WM, WN, AC, BC, S, E, H>>& sums) {
-  ring_tile(A, B, k0, k1, smem, sums);
 }
 
 }  // namespace pinsage
