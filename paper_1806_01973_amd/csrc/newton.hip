@@ -277,29 +277,167 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch
   }
 }
 
+// ---- matrices in LDS -------------------------------------------------------------------
+// Rows of 16-bit values in parts, 16-byte slot s of row r at s ^ lds_swizzle(r): a fragment
+// read's 8 rows, and the 4 rows of a transposing read, fall on distinct banks.
+__device__ __forceinline__ int lds_swizzle(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
+
+// Eight k of each of 32 rows from r0 on: step ks of 16.
+template <int PLANES>
+__device__ __forceinline__ Parts8<PLANES> lds_fragment(const unsigned char* M, int pitch, int plane,
+                                                       int r0, int ks) {
+  const int lane = threadIdx.x & 63, r = r0 + (lane & 31);
+  Parts8<PLANES> f;
+#pragma unroll
+  for (int p = 0; p < PLANES; ++p)
+    f.p[p] = *reinterpret_cast<const u32x4*>(M + p * plane + r * pitch +
+                                             (((2 * ks + (lane >> 5)) ^ lds_swizzle(r)) * 16));
+  return f;
+}
+template <int PLANES>
+__device__ __forceinline__ void multiply_parts(const Parts8<PLANES>& b, const Parts8<PLANES>& l,
+                                               f32x16& acc) {
+  constexpr int MODE = PLANES == 2 ? kF16x2 : kF16;
+  if constexpr (PLANES == 2) {
+    acc = product_mfma<MODE>(b.p[PLANES - 1], l.p[0], acc);
+    acc = product_mfma<MODE>(b.p[0], l.p[PLANES - 1], acc);
+  }
+  acc = product_mfma<MODE>(b.p[0], l.p[0], acc);
+}
+
+// ---- medium matrices: A's square and its product with Y in one launch -------------------
+// Y (a I + b A + c A A) = a Y + b T + c T A with T = Y A: a block holds A and 32 rows of Y in
+// LDS, forms T in Y's place (rounded as Y is) and Y's successor from it. Against the two
+// launches (B, then Y B) it multiplies more, 4 m^2 n against m^3 + 2 m^2 n, but up to 256
+// columns (128 in two parts), where A fits beside Y, launches and loads are what costs:
+// 6.5 us for 8 matrices of 256 x 512 where the two take 9.3. Whole calls in us, with it
+// and without: bf16 128 x 512 56, 71; 4 of 100 x 1,000 66, 82; 8 of 256 x 512 69, 80; 8 of
+// 256 x 2,048 127, 129; fp32 128 x 512 76, 95; 8 of 128 x 2,048 147, 162. The width is a
+// compile-time constant: at run time its divisions alone took 3 us.
+constexpr int kBandWaves = 8, kBandRows = 32;
+
+template <int PLANES, int mp>
+__global__ __launch_bounds__(64 * kBandWaves) void newton_band_kernel(NewtonLaunch a, NewtonWork w,
+                                                                      int from) {
+  constexpr int THREADS = 64 * kBandWaves, slots = mp / 8, pitch = mp * 2;
+  constexpr int plane_a = mp * pitch, plane_y = kBandRows * pitch;
+  __shared__ __attribute__((aligned(16))) unsigned char smem[PLANES * (plane_a + plane_y)];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int bands = w.np / kBandRows, id = xcd_tile(blockIdx.x, gridDim.x);
+  const int64_t z = id / bands, i0 = (int64_t)(id % bands) * kBandRows;
+  const int64_t px = (int64_t)mp * w.np, pa = (int64_t)mp * mp;
+  const uint16_t* const Y = w.Y[from] + z * PLANES * px + i0 * mp;
+  uint16_t* const out = w.Y[1 - from] + z * PLANES * px + i0 * mp;
+  const uint16_t* const A = w.A + z * PLANES * pa;
+  unsigned char* const lds_a = smem;                          // planes of mp rows
+  unsigned char* const lds_y = smem + PLANES * plane_a;       // planes of 32 rows
+  auto at = [&](unsigned char* M, int r, int slot) __attribute__((always_inline)) {
+    return reinterpret_cast<u32x4*>(M + r * pitch + ((slot ^ lds_swizzle(r)) * 16));
+  };
+  constexpr int VECTORS = PLANES * mp * slots, BATCH = (VECTORS + THREADS - 1) / THREADS;
+  u32x4 v[BATCH];  // all of a thread's loads in flight
+#pragma unroll
+  for (int u = 0; u < BATCH; ++u) {
+    const int q = tid + u * THREADS;
+    if (VECTORS % THREADS == 0 || q < VECTORS) v[u] = *reinterpret_cast<const u32x4*>(A + q * 8);
+  }
+#pragma unroll
+  for (int u = 0; u < BATCH; ++u) {
+    const int q = tid + u * THREADS, row = q / slots;  // of all planes
+    if (VECTORS % THREADS == 0 || q < VECTORS)
+      *at(lds_a + row / mp * plane_a, row % mp, q % slots) = v[u];
+  }
+  for (int q = tid; q < PLANES * kBandRows * slots; q += THREADS) {
+    const int p = q / (kBandRows * slots), e = q % (kBandRows * slots);
+    *at(lds_y + p * plane_y, e / slots, e % slots) =
+        *reinterpret_cast<const u32x4*>(Y + p * px + e * 8);
+  }
+  __syncthreads();
+
+  // A wave's 32 columns; waves past the last one only load and wait.
+  const bool works = 32 * wave < mp;
+  const int i = lane & 31;
+  const float back = 1.0f / kScale;  // products carry the scale twice
+  f32x16 acc;
+  auto product = [&]() __attribute__((always_inline)) {
+    clear_block(acc);
+#pragma unroll
+    for (int ks = 0; ks < mp / 16; ++ks)
+      multiply_parts<PLANES>(lds_fragment<PLANES>(lds_a, pitch, plane_a, 32 * wave, ks),
+                             lds_fragment<PLANES>(lds_y, pitch, plane_y, 0, ks), acc);
+  };
+  // The lane's columns 8 g + 4 (lane / 32) of the wave's, row i of the band.
+  auto place = [&](int g) __attribute__((always_inline)) {
+    const int j = 32 * wave + 8 * g + 4 * (lane >> 5);
+    return reinterpret_cast<uint16_t*>(lds_y + i * pitch + (((j >> 3) ^ lds_swizzle(i)) * 16) +
+                                       (j & 4) * 2);
+  };
+  float sum[16];
+  if (works) {
+    product();
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const uint2 hi = *reinterpret_cast<const uint2*>(place(g));
+      uint2 lo = make_uint2(0, 0);
+      if constexpr (PLANES == 2) lo = *reinterpret_cast<const uint2*>(place(g) + plane_y / 2);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float y = unpack_f16(e < 2 ? hi.x : hi.y, e & 1);
+        if constexpr (PLANES == 2) y += unpack_f16(e < 2 ? lo.x : lo.y, e & 1);
+        sum[4 * g + e] = fmaf(a.a, y, a.b * back * acc[4 * g + e]);
+      }
+    }
+  }
+  __syncthreads();  // all have read Y
+  if (works)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      float t[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) t[e] = back * acc[4 * g + e];
+      put<PLANES>(place(g), plane_y / 2, t);
+    }
+  __syncthreads();
+  if (works) product();
+  __syncthreads();  // all have read T
+  if (works)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      float y[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = fmaf(a.c * back, acc[4 * g + e], sum[4 * g + e]);
+      put<PLANES>(place(g), plane_y / 2, y);
+    }
+  __syncthreads();
+  for (int q = tid; q < PLANES * kBandRows * slots; q += THREADS) {
+    const int p = q / (kBandRows * slots), e = q % (kBandRows * slots);
+    *reinterpret_cast<u32x4*>(out + p * px + e * 8) =
+        *at(lds_y + p * plane_y, e / slots, e % slots);
+  }
+}
+
 // ---- small matrices: everything in one block ------------------------------------------
 // A block of eight waves takes a matrix from G to the result, X and one m x m matrix in
-// its LDS: what bounds the launches above for small matrices is that there are 17 of
-// them, at 3 to 5 us each whatever they compute. In two parts always. Up to 64 x 384, and
-// in fp32 128 x 128, measured, us, one block / launches: 64 x 64 26 / 59 (bf16 53), 512 of
-// them 54 / 113, 300 x 40 50 / 75, 128 x 128 72 / 79 (bf16 64), 64 x 512 98 / 84.
-// X [mp][np] and A [mp][mp] lie in LDS in fp16 parts, 16-byte slot s of row r at
-// s ^ small_swizzle(r): a fragment read's 8 rows, and the 4 rows of a transposing read
-// (X's columns, for B X), fall on distinct banks. A wave's blocks of 32 x 32 stay in its
-// accumulators until all waves have read what they replace.
+// its LDS: what bounds a small matrix else is that there are 13 launches, at 3 to 5 us
+// each whatever they compute. In two parts always. Up to 64 x 320, us, one block and
+// launches: 64 x 64 25, 49; 512 of them 53, 84; 300 x 40 49, 60; 64 x 320 58, 61;
+// 64 x 384 67, 63; fp32 128 x 128 72, 63.
+// X [mp][np] and A [mp][mp] lie in LDS in fp16 parts; X's columns, for B X, come through
+// transposing reads. A wave's blocks of 32 x 32 stay in its accumulators until all waves
+// have read what they replace.
 constexpr int kSmallWaves = 8, kSmallBlocks = 3;  // blocks per wave at most, of X or A
-constexpr int kSmallLds = 128 * 1024;
+constexpr int kSmallSide = 64, kSmallLong = 320;
+constexpr int kSmallLds = 2 * 2 * kSmallSide * (kSmallLong + kSmallSide);
 
-__device__ __forceinline__ int small_swizzle(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
-
-inline bool fits_one_block(const NewtonWork& w, bool bf16) {
-  return (w.mp == 64 && w.np <= 384) || (!bf16 && w.mp == 128 && w.np == 128);
+inline bool fits_one_block(const NewtonWork& w) {
+  return w.mp == kSmallSide && w.np <= kSmallLong;
 }
 
 template <bool BF16>
 __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLaunch a,
                                                                         NewtonWork w) {
-  constexpr int PLANES = 2, MODE = kF16x2, THREADS = 64 * kSmallWaves;
+  constexpr int PLANES = 2, THREADS = 64 * kSmallWaves;
   __shared__ __attribute__((aligned(16))) unsigned char smem[kSmallLds];
   __shared__ double norms[kSmallWaves];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -352,7 +490,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
     for (int e = 0; e < 4; ++e) {
       if (e >= cols) break;
       const int i = w.flip ? c + e : r, j = w.flip ? r : c + e;
-      unsigned char* const to = X + i * np * 2 + (((j >> 3) ^ small_swizzle(i)) * 16) + (j & 7) * 2;
+      unsigned char* const to = X + i * np * 2 + (((j >> 3) ^ lds_swizzle(i)) * 16) + (j & 7) * 2;
       const float v = (float)(u[e] * inv);
       const _Float16 hi = (_Float16)v;
       *reinterpret_cast<_Float16*>(to) = hi;
@@ -362,22 +500,9 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
   __syncthreads();
 
   const int frag_row = lane & 31, half = lane >> 5;
-  struct Frag {
-    u32x4 p[PLANES];
-  };
-  auto row_frag = [&](const unsigned char* M, int pitch, int plane, int r0, int ks)
-      __attribute__((always_inline)) {
-    Frag f;
-    const int r = r0 + frag_row;
-#pragma unroll
-    for (int p = 0; p < PLANES; ++p)
-      f.p[p] = *reinterpret_cast<const u32x4*>(M + p * plane + r * pitch +
-                                               (((2 * ks + half) ^ small_swizzle(r)) * 16));
-    return f;
-  };
   // Columns c0 .. c0 + 31 of X, k along its rows.
   auto col_frag = [&](int c0, int ks) __attribute__((always_inline)) {
-    Frag f;
+    Parts8<PLANES> f;
     const int c = c0 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
 #pragma unroll
     for (int p = 0; p < PLANES; ++p)
@@ -385,7 +510,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
       for (int h = 0; h < 2; ++h) {
         const int k = 16 * ks + 8 * half + 4 * h + ((lane >> 2) & 3);
         const unsigned char* const at =
-            X + p * px + k * np * 2 + (((c >> 3) ^ small_swizzle(k)) * 16) + (c & 4) * 2;
+            X + p * px + k * np * 2 + (((c >> 3) ^ lds_swizzle(k)) * 16) + (c & 4) * 2;
         const u32x2 x = __builtin_bit_cast(
             u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                        (__attribute__((address_space(3))) s16x4*)at));
@@ -393,13 +518,6 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
         f.p[p][2 * h + 1] = x[1];
       }
     return f;
-  };
-  auto multiply = [&](const Frag& b, const Frag& l, f32x16& acc) __attribute__((always_inline)) {
-    if constexpr (PLANES == 2) {
-      acc = product_mfma<MODE>(b.p[PLANES - 1], l.p[0], acc);
-      acc = product_mfma<MODE>(b.p[0], l.p[PLANES - 1], acc);
-    }
-    acc = product_mfma<MODE>(b.p[0], l.p[0], acc);
   };
   // Block (bi, bj) of M becomes p M + q sum.
   auto update = [&](unsigned char* M, int pitch, int plane, int bi, int bj, float p, float q,
@@ -409,7 +527,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
     for (int g = 0; g < 4; ++g) {
       const int j = 32 * bj + 8 * g + 4 * half;
       uint16_t* const at = reinterpret_cast<uint16_t*>(
-          M + i * pitch + (((j >> 3) ^ small_swizzle(i)) * 16) + (j & 4) * 2);
+          M + i * pitch + (((j >> 3) ^ lds_swizzle(i)) * 16) + (j & 4) * 2);
       float v[4];
       if (p == 0.0f) {
 #pragma unroll
@@ -438,7 +556,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
       const int bi = b / mb, bj = b % mb;
       clear_block(acc[0]);
       for (int ks = 0; ks < np / 16; ++ks)
-        multiply(row_frag(X, np * 2, px, 32 * bj, ks), row_frag(X, np * 2, px, 32 * bi, ks), acc[0]);
+        multiply_parts<PLANES>(lds_fragment<PLANES>(X, np * 2, px, 32 * bj, ks), lds_fragment<PLANES>(X, np * 2, px, 32 * bi, ks), acc[0]);
       update(A, mp * 2, pa, bi, bj, 0.0f, back, acc[0]);
     }
     __syncthreads();
@@ -450,8 +568,8 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
       for (int t = 0; t < kSmallBlocks; ++t) {
         const int b = wave + t * kSmallWaves;
         if (b < mb * mb)
-          multiply(row_frag(A, mp * 2, pa, 32 * (b % mb), ks),
-                   row_frag(A, mp * 2, pa, 32 * (b / mb), ks), acc[t]);
+          multiply_parts<PLANES>(lds_fragment<PLANES>(A, mp * 2, pa, 32 * (b % mb), ks),
+                   lds_fragment<PLANES>(A, mp * 2, pa, 32 * (b / mb), ks), acc[t]);
       }
     __syncthreads();
 #pragma unroll
@@ -468,7 +586,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
       for (int t = 0; t < kSmallBlocks; ++t) {
         const int b = wave + t * kSmallWaves;
         if (b < mb * nb)
-          multiply(col_frag(32 * (b / mb), ks), row_frag(A, mp * 2, pa, 32 * (b % mb), ks), acc[t]);
+          multiply_parts<PLANES>(col_frag(32 * (b / mb), ks), lds_fragment<PLANES>(A, mp * 2, pa, 32 * (b % mb), ks), acc[t]);
       }
     __syncthreads();
 #pragma unroll
@@ -491,7 +609,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
       v[e] = 0.0f;
       if (e < cols) {
         const unsigned char* const from =
-            X + i * np * 2 + (((j >> 3) ^ small_swizzle(i)) * 16) + (j & 7) * 2;
+            X + i * np * 2 + (((j >> 3) ^ lds_swizzle(i)) * 16) + (j & 7) * 2;
         v[e] = (float)*reinterpret_cast<const _Float16*>(from);
         if constexpr (PLANES == 2) v[e] += (float)*reinterpret_cast<const _Float16*>(from + px);
       }
@@ -576,19 +694,36 @@ size_t layout(int64_t batch, int rows, int cols, bool bf16, unsigned char* ws, N
 }
 
 // The padded sides of a small matrix, whatever its batch asks of the launches.
-bool one_block(const NewtonLaunch& a, NewtonWork* w) {
+bool one_block(NewtonWork* w) {
   NewtonWork one = *w;
   one.mp = (w->m + 63) / 64 * 64;
   one.np = (w->n + 63) / 64 * 64;
-  if (!fits_one_block(one, a.bf16)) return false;
+  if (!fits_one_block(one)) return false;
   *w = one;
   return true;
+}
+
+template <int PLANES, int MP>
+bool launch_band_of(const NewtonLaunch& a, const NewtonWork& w, int from, hipStream_t s) {
+  if (w.mp != MP) return false;
+  hipLaunchKernelGGL((newton_band_kernel<PLANES, MP>),
+                     dim3((unsigned)(w.np / kBandRows * a.batch)), dim3(64 * kBandWaves), 0, s, a, w,
+                     from);
+  return true;
+}
+template <int PLANES>
+bool launch_band(const NewtonLaunch& a, const NewtonWork& w, int from, hipStream_t s) {
+  if constexpr (PLANES == 1)
+    return launch_band_of<1, 128>(a, w, from, s) || launch_band_of<1, 192>(a, w, from, s) ||
+           launch_band_of<1, 256>(a, w, from, s);
+  else
+    return launch_band_of<2, 64>(a, w, from, s) || launch_band_of<2, 128>(a, w, from, s);
 }
 
 template <bool BF16, int PLANES>
 hipError_t launch_parts(const NewtonLaunch& a, NewtonWork w, hipStream_t s) {
   const unsigned batch = (unsigned)a.batch;
-  if (one_block(a, &w)) {
+  if (one_block(&w)) {
     hipLaunchKernelGGL(newton_small_kernel<BF16>, dim3(batch), dim3(64 * kSmallWaves), 0, s, a, w);
     return hipGetLastError();
   }
@@ -598,6 +733,7 @@ hipError_t launch_parts(const NewtonLaunch& a, NewtonWork w, hipStream_t s) {
                      dim3((unsigned)(w.mp / 64), (unsigned)(w.np / 64), batch), dim3(256), 0, s, a, w);
   for (int k = 0, from = 0; k < a.steps; ++k, from = 1 - from) {
     launch_product<kGram, BF16, PLANES>(a, w, from, s);
+    if (k + 1 < a.steps && launch_band<PLANES>(a, w, from, s)) continue;
     launch_product<kSquare, BF16, PLANES>(a, w, from, s);
     if (k + 1 < a.steps) launch_product<kApply, BF16, PLANES>(a, w, from, s);
     else launch_product<kLast, BF16, PLANES>(a, w, from, s);
