@@ -78,7 +78,8 @@ __device__ __forceinline__ float value(const Parts8<PLANES>& x, int e) {
 
 // ---- the norm, with the momentum's update ---------------------------------------
 // What is orthogonalised, elements at .. at + 3 of the batch's storage: the input,
-// or the step's combination of it with the already updated momentum.
+// or the step's combination of it with the already updated momentum. The norm of
+// 2,048 x 2,048 bf16 with its momentum takes 9 us (42 MB, 4.7 TB/s), Y0 9 us.
 template <bool BF16>
 __device__ __forceinline__ void update4(const NewtonLaunch& a, int64_t at, int cols, float (&u)[4]) {
   read_row<BF16>(a.in, at, cols, u);
@@ -165,7 +166,11 @@ __global__ __launch_bounds__(256) void newton_start_kernel(NewtonLaunch a, Newto
 // ---- the three products -----------------------------------------------------------
 enum NewtonProduct { kGram = 0, kSquare = 1, kApply = 2, kLast = 3 };
 
-// P[i][j] = sum_k L(i, k) R(j, k): Y^T Y, A A, or Y B (A and B are symmetric).
+// P[i][j] = sum_k L(i, k) R(j, k): Y^T Y, A A, or Y B (A and B are symmetric). About 8 us
+// of each are its launch, first loads and epilogue; the rest is bound by what the tiles
+// load (64 x 64: 16 to 20 TB/s out of the L2s; order of tiles and row pitch make no
+// difference). 2,048 x 2,048 in one part 24, 23 and 26 us (the last 660 TFLOP/s), 2,048 x
+// 1,024 in two parts 20, 12 and 19 us.
 template <class C, int KIND, bool BF16>
 __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch a, NewtonWork w,
                                                                     int from, int tiles) {

@@ -241,6 +241,42 @@ def test_strides_and_offsets_of_rows(n, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,d_in,d_out", [
+    (40, 7, 3), (200, 3, 67), (200, 67, 5), (150, 131, 71), (150, 9, 129), (700, 15, 15),
+    (300, 64, 65), (300, 65, 64), (9000, 301, 131), (9000, 131, 301), (20_000, 257, 259)])
+def test_nothing_around_the_operands_is_used(n, d_in, d_out, dtype):
+    """Rows that end inside a 16-byte vector, at odd addresses, with NaN before and
+    behind every row and around the whole operand."""
+    x, W, b, dy, _ = make(n, d_in, d_out, dtype, seed=12)
+
+    def among_nan(t):
+        wide = torch.full((t.shape[0] + 2, t.shape[1] + 9), math.nan, dtype=t.dtype, device="cuda")
+        view = wide[1:-1, 3:3 + t.shape[1]]
+        view.copy_(t)
+        return view
+
+    xs, Ws, dys = among_nan(x), among_nan(W), among_nan(dy)
+    out = ps().dense_forward(xs, Ws, b.cuda(), "silu", residual=dys)
+    check_forward(x, W, b, dy, None, "silu", dtype, out)
+    u = pre64(x, W, b, None)[0].to(DT[dtype])
+    got = ps().dense_backward(dys, xs, Ws, among_nan(u), "silu")
+    check_backward(x, W, u, dy, None, "silu", dtype, *got)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sizes,d_in,d_out", [
+    ([150, 0, 3, 700], 37, 69), ([64, 65, 1, 2000], 130, 5), ([3000, 0, 2500], 75, 141)])
+def test_grouped_layers_of_odd_widths(sizes, d_in, d_out, dtype):
+    n = sum(sizes)
+    x, W, b, dy, off = make(n, d_in, d_out, dtype, len(sizes), sizes, seed=13)
+    y = ps().dense_forward(x.cuda(), W.cuda(), b.cuda(), "gelu", offsets=off.cuda())
+    check_forward(x, W, b, None, off, "gelu", dtype, y)
+    u = pre64(x, W, b, off)[0].to(DT[dtype])
+    got = ps().dense_backward(dy.cuda(), x.cuda(), W.cuda(), u.cuda(), "gelu", offsets=off.cuda())
+    check_backward(x, W, u, dy, off, "gelu", dtype, *got)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_residual_in_place(dtype):
     x, W, b, r, _ = make(500, 64, 96, dtype, seed=6)
     y = r.cuda()

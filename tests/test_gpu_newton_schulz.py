@@ -67,6 +67,21 @@ def test_orthogonalize(shape, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(2, 64, 320), (2, 321, 64), (1, 700, 33), (3, 65, 66), (3, 192, 191),
+                                   (1, 193, 256), (2, 256, 257), (1, 97, 2000), (9, 128, 129)])
+def test_sides_around_the_kernels_limits(shape, dtype):
+    g = gradient(shape, seed=sum(shape)).to(DT[dtype])
+    if shape[0] > 2:
+        g[1] = float("nan")  # stays in its matrix
+    out, want = ps().orthogonalize(g.cuda()), newton64(g)
+    for i in range(shape[0]):
+        if g[i].isnan().any():
+            assert out[i].isnan().all(), i
+        else:
+            assert off(out[i], want[i]) <= TOL[dtype], i
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_one_matrix_without_a_batch_and_in_place(dtype):
     g = gradient((90, 70), 1).to(DT[dtype])
     want = newton64(g)
