@@ -299,11 +299,15 @@ __device__ __forceinline__ Parts8<PLANES> lds_fragment(const unsigned char* M, i
                                              (((2 * ks + (lane >> 5)) ^ lds_swizzle(r)) * 16));
   return f;
 }
+// All products of the parts, lo lo too: the diagonal of A sums squares, so what is left
+// out has one sign, which shows with few singular values (fp32, 16 x 100, 4 draws: mean
+// error 1.3e-6, with lo lo 1.0e-6).
 template <int PLANES>
 __device__ __forceinline__ void multiply_parts(const Parts8<PLANES>& b, const Parts8<PLANES>& l,
                                                f32x16& acc) {
   constexpr int MODE = PLANES == 2 ? kF16x2 : kF16;
   if constexpr (PLANES == 2) {
+    acc = product_mfma<MODE>(b.p[PLANES - 1], l.p[PLANES - 1], acc);
     acc = product_mfma<MODE>(b.p[PLANES - 1], l.p[0], acc);
     acc = product_mfma<MODE>(b.p[0], l.p[PLANES - 1], acc);
   }
