@@ -560,9 +560,10 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void dense_dw_kernel(DenseGradL
 // dx and dW in one launch, dW's blocks first: for few rows a launch costs as much as
 // either (about 5 us). A whole backward pass, together against apart: 1,000 rows of
 // 256 -> 256 20.0 and 22.2 us (bf16), 20.1 and 27.8 (fp32); 4,596 of 512 -> 512 31.9
-// and 35.5, 61.5 and 67.9. With many blocks the two only take cache from each other
+// and 35.5, 61.5 and 67.9; up to 1,280 blocks, five a CU (4,596 of 512 -> 256, 1,056
+// blocks, 25.5 and 28.0, fp32 42.8 and 48.8). With many blocks the two only take cache from each other
 // (60,000 x 1,024 -> 512 in 64 equal groups 220 us, apart 108 + 80).
-constexpr int64_t kGradsTogether = 1024;
+constexpr int64_t kGradsTogether = 1280;
 template <class CX, class CW>
 __global__ __launch_bounds__(CX::THREADS, CX::WPE) void dense_grads_kernel(DenseLaunch x,
                                                                            DenseGradLaunch w,
