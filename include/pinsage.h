@@ -555,11 +555,13 @@ int pinsage_dense_backward(const pinsage_dense_t* layer, const void* dy, int64_t
  *   A = X X^T,  X = a X + (b A + c A A) X,
  * returned in G's orientation: for (a, b, c) = (3.4445, -4.7750, 2.0315) and 5
  * steps, singular values above about 0.01 of the norm end between 0.7 and 1.2.
- * A zero matrix stays zero (eps > 0). Products on fp16 parts around a fixed
- * scale: one part (2^-11) for bf16 storage, two (2^-22) for fp32 and for bf16
- * where m <= 64; coefficients
- * must keep X, A and b A + c A A below 16 in magnitude, as those above do, and
- * a matrix whose norm is far below eps loses low bits (absolute 2^-36 of X).
+ * A zero matrix stays zero (eps > 0). X, A and b A + c A A are held to 2^-23 of
+ * themselves (two fp16 parts around a fixed scale), whatever the storage type; the
+ * steps enlarge small singular directions about 480 times and these roundings with
+ * them (fp32, rank 1: 2.7e-5 of the result, where the formula in fp32 leaves
+ * 1.3e-4). Coefficients must keep X, A, b A + c A A and A X below 16 in magnitude,
+ * as those above do, and a matrix whose norm is far below eps loses low bits
+ * (absolute 2^-36 of X).
  * Limits: 1 <= rows, cols <= 16384, 1 <= steps <= 64, batch <= 65535. */
 typedef struct {
   int64_t batch;

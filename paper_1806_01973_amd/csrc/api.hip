@@ -1936,8 +1936,7 @@ int pinsage_newton_schulz_workspace_size(const pinsage_newton_schulz_t* params, 
   *bytes = 0;
   const int st = check_newton(params);
   if (st) return st;
-  *bytes = newton_workspace(params->batch, params->rows, params->cols,
-                            params->dtype == PINSAGE_BF16);
+  *bytes = newton_workspace(params->batch, params->rows, params->cols);
   return PINSAGE_OK;
 }
 
@@ -1949,8 +1948,7 @@ int pinsage_orthogonalize(const pinsage_newton_schulz_t* params, const void* in,
   if (params->batch == 0) return PINSAGE_OK;
   if (!in || !out) return fail(PINSAGE_EINVAL, "in or out is NULL");
   const NewtonLaunch a = newton_launch(params, in, out);
-  if ((st = check_workspace(workspace, workspace_bytes,
-                            newton_workspace(a.batch, a.rows, a.cols, a.bf16))))
+  if ((st = check_workspace(workspace, workspace_bytes, newton_workspace(a.batch, a.rows, a.cols))))
     return st;
   const hipError_t e = launch_newton(a, workspace, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? PINSAGE_OK : hip_fail(e, "orthogonalisation launch");
@@ -1977,8 +1975,7 @@ int pinsage_muon_step(const pinsage_newton_schulz_t* params, const pinsage_muon_
   a.decay = (float)(1.0 - (double)muon->lr * muon->weight_decay);
   a.rate = muon->lr * muon->scale;
   a.nesterov = muon->nesterov != 0;
-  if ((st = check_workspace(workspace, workspace_bytes,
-                            newton_workspace(a.batch, a.rows, a.cols, a.bf16))))
+  if ((st = check_workspace(workspace, workspace_bytes, newton_workspace(a.batch, a.rows, a.cols))))
     return st;
   const hipError_t e = launch_newton(a, workspace, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? PINSAGE_OK : hip_fail(e, "optimiser step launch");

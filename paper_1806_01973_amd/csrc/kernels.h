@@ -340,7 +340,7 @@ hipError_t launch_dense_dx_dw(const DenseLaunch& x, const DenseGradLaunch& w, hi
 hipError_t launch_dense_join(const DenseGradLaunch& a, hipStream_t s);
 
 // Newton-Schulz orthogonalisation of `batch` matrices [rows][cols] (contiguous), and
-// the optimiser step around it (newton.hip). `update` null: X0 = in / (|in| + eps).
+// the optimiser step around it (newton.hip).
 struct NewtonLaunch {
   const void* in;  // storage dtype
   void* out;       // storage dtype: the result, or the new weight
@@ -359,7 +359,7 @@ struct NewtonLaunch {
   float beta = 0, decay = 0, rate = 0;
   bool nesterov = false;
 };
-size_t newton_workspace(int64_t batch, int rows, int cols, bool bf16);
+size_t newton_workspace(int64_t batch, int rows, int cols);
 hipError_t launch_newton(const NewtonLaunch& a, void* workspace, hipStream_t s);
 
 // Frontier machinery of the minibatch forward (node flags + exclusive scan).

@@ -5,13 +5,13 @@
 // which moves every singular value of X towards 1.
 //
 // Every singular value of X stays near [0, 1.3], so all intermediates fit fp16
-// around a fixed scale 2^12 (values to 16, the smallest normal 2^-26): bf16
-// storage keeps them as one fp16 value each (2^-11 instead of bf16's 2^-8; the
-// result rounds to bf16 once, at the end), fp32 storage as two (22 significand
-// bits, three MFMAs a product, against six for bf16 parts). With few singular
-// values the roundings of one part do not average out (error 2.4e-3 on average
-// and 4e-3 at worst for m = 1 .. 16, against 1.7e-3 of bf16's own and 2.2e-3 in all
-// for m >= 100), so up to 64 bf16 storage takes two parts as well. Sums, and a X, run in
+// around a fixed scale 2^12 (values to 16, the smallest normal 2^-26). They are kept as
+// two fp16 parts (22 significand bits, three MFMAs a product, against six for bf16
+// parts), whatever the storage type. Five steps enlarge small singular directions about
+// 480 times, and what is rounded off X, A and B in their place with them: of a bf16
+// matrix of rank 1 (16) one part's 2^-11 leaves an error of 9.5e-2 (3.8e-2), two parts
+// 1.6e-3 as the formula in fp32 does, which is bf16's own rounding of the result. fp32
+// of rank 1: 2.7e-5, the formula in fp32 1.3e-4. Sums, and a X, run in
 // fp32; |G|_F is summed in fp64, so no finite G overflows.
 // Y = X^T, A and B live in the workspace, padded with zeros to whole tiles, so that
 // no product has an edge: A = Y^T Y (both operands by columns), A A, and
@@ -24,17 +24,17 @@ namespace pinsage {
 namespace {
 
 constexpr float kScale = 4096.0f;  // the stored values over the true ones
+constexpr int kParts = 2;          // fp16 parts of a stored value
 constexpr int kMaxNormBlocks = 1024;  // partial sums of a matrix's norm
 
 struct NewtonWork {
   double* norms;     // [batch][kMaxNormBlocks]
-  uint16_t* Y[2];    // [batch][planes][np][mp]
-  uint16_t* A;       // [batch][planes][mp][mp]
+  uint16_t* Y[2];    // [batch][kParts][np][mp]
+  uint16_t* A;       // [batch][kParts][mp][mp]
   uint16_t* B;
   int m, n, mp, np;  // m <= n; padded
   int norm_blocks;
   bool flip;         // X is G^T
-  bool two;          // two fp16 parts
 };
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -45,35 +45,30 @@ __device__ __forceinline__ float unpack_f16(uint32_t w, int h) {
   return (float)__builtin_bit_cast(f16x2, w)[h];
 }
 
-// Stores N scaled values as one or two fp16 parts; p on 2 N bytes.
-template <int PLANES, int N>
+// Stores N scaled values as two fp16 parts; p on 2 N bytes.
+template <int N>
 __device__ __forceinline__ void put(uint16_t* p, int64_t plane, const float (&v)[N]) {
   typedef uint32_t words __attribute__((ext_vector_type(N / 2)));
   words hi, lo;
 #pragma unroll
   for (int e = 0; e < N / 2; ++e) {
     hi[e] = pack_f16(v[2 * e], v[2 * e + 1]);
-    if constexpr (PLANES == 2)
-      lo[e] = pack_f16(v[2 * e] - unpack_f16(hi[e], 0), v[2 * e + 1] - unpack_f16(hi[e], 1));
+    lo[e] = pack_f16(v[2 * e] - unpack_f16(hi[e], 0), v[2 * e + 1] - unpack_f16(hi[e], 1));
   }
   *reinterpret_cast<words*>(p) = hi;
-  if constexpr (PLANES == 2) *reinterpret_cast<words*>(p + plane) = lo;
+  *reinterpret_cast<words*>(p + plane) = lo;
 }
-template <int PLANES>
 struct Parts8 {
-  u32x4 p[PLANES];
+  u32x4 p[kParts];
 };
-template <int PLANES>
-__device__ __forceinline__ Parts8<PLANES> get8(const uint16_t* p, int64_t plane) {
-  Parts8<PLANES> x;
+__device__ __forceinline__ Parts8 get8(const uint16_t* p, int64_t plane) {
+  Parts8 x;
   x.p[0] = *reinterpret_cast<const u32x4*>(p);
-  if constexpr (PLANES == 2) x.p[1] = *reinterpret_cast<const u32x4*>(p + plane);
+  x.p[1] = *reinterpret_cast<const u32x4*>(p + plane);
   return x;
 }
-template <int PLANES>
-__device__ __forceinline__ float value(const Parts8<PLANES>& x, int e) {
-  const float hi = unpack_f16(x.p[0][e / 2], e & 1);
-  return PLANES == 2 ? hi + unpack_f16(x.p[PLANES - 1][e / 2], e & 1) : hi;
+__device__ __forceinline__ float value(const Parts8& x, int e) {
+  return unpack_f16(x.p[0][e / 2], e & 1) + unpack_f16(x.p[1][e / 2], e & 1);
 }
 
 // ---- the norm, with the momentum's update ---------------------------------------
@@ -124,7 +119,7 @@ __global__ __launch_bounds__(256) void newton_norm_kernel(NewtonLaunch a, Newton
 }
 
 // ---- Y0: scaled, in fp16 parts, padded ---------------------------------------------
-template <bool BF16, int PLANES>
+template <bool BF16>
 __global__ __launch_bounds__(256) void newton_start_kernel(NewtonLaunch a, NewtonWork w) {
   __shared__ float tile[64][65];
   __shared__ double part[4];
@@ -152,14 +147,14 @@ __global__ __launch_bounds__(256) void newton_start_kernel(NewtonLaunch a, Newto
   }
   __syncthreads();
   const int64_t plane = (int64_t)w.mp * w.np;
-  uint16_t* const Y = w.Y[0] + blockIdx.z * PLANES * plane;
+  uint16_t* const Y = w.Y[0] + blockIdx.z * kParts * plane;
 #pragma unroll
   for (int q = tid; q < 64 * 8; q += 256) {
     const int i = q / 8, j = q % 8 * 8;
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = w.flip ? tile[i][j + e] : tile[j + e][i];
-    put<PLANES>(Y + (int64_t)(i0 + i) * w.mp + j0 + j, plane, v);
+    put(Y + (int64_t)(i0 + i) * w.mp + j0 + j, plane, v);
   }
 }
 
@@ -175,15 +170,15 @@ template <class C, int KIND, bool BF16>
 __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch a, NewtonWork w,
                                                                     int from, int tiles) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[C::LDS_BYTES];
-  constexpr int PLANES = C::MEM_PLANES;
+  static_assert(C::MEM_PLANES == kParts, "");
   constexpr bool kSymmetric = KIND == kGram || KIND == kSquare;
   const int64_t px = (int64_t)w.mp * w.np, pa = (int64_t)w.mp * w.mp;
   // Neighbouring tiles, and whole matrices of a batch, on one XCD.
   const int id = xcd_tile(blockIdx.x, gridDim.x), tile = id % tiles;
   const int64_t z = id / tiles;
-  const uint16_t* const Y = w.Y[from] + z * PLANES * px;
-  uint16_t* const A = w.A + z * PLANES * pa;
-  uint16_t* const B = w.B + z * PLANES * pa;
+  const uint16_t* const Y = w.Y[from] + z * kParts * px;
+  uint16_t* const A = w.A + z * kParts * pa;
+  uint16_t* const B = w.B + z * kParts * pa;
   int ti, tj;
   if constexpr (kSymmetric) {
     // Tiles on and above the diagonal, row by row.
@@ -221,7 +216,7 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch
         sums, smem,
         [&](int m, int n) __attribute__((always_inline)) {
           if constexpr (KIND == kGram) return Nothing{};
-          else return get8<PLANES>(A + (int64_t)(i0 + m) * w.mp + j0 + n, pa);
+          else return get8(A + (int64_t)(i0 + m) * w.mp + j0 + n, pa);
         },
         [&](int m, int n, float (&v)[8], const auto& x) __attribute__((always_inline)) {
 #pragma unroll
@@ -229,23 +224,23 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch
             if constexpr (KIND == kGram) v[e] *= back;
             else v[e] = fmaf(a.b, value(x, e), a.c * back * v[e]);
           }
-          put<PLANES>(out + (int64_t)(i0 + m) * w.mp + j0 + n, pa, v);
+          put(out + (int64_t)(i0 + m) * w.mp + j0 + n, pa, v);
         },
         [&](int m, int n, const float (&v)[8]) __attribute__((always_inline)) {
-          put<PLANES>(out + (int64_t)(j0 + n) * w.mp + i0 + m, pa, v);
+          put(out + (int64_t)(j0 + n) * w.mp + i0 + m, pa, v);
         },
         ti != tj);
   } else if constexpr (KIND == kApply) {
-    uint16_t* const out = w.Y[1 - from] + z * PLANES * px;
+    uint16_t* const out = w.Y[1 - from] + z * kParts * px;
     product_rows_cols<8>(
         sums, smem,
         [&](int m, int n) __attribute__((always_inline)) {
-          return get8<PLANES>(Y + (int64_t)(i0 + m) * w.mp + j0 + n, px);
+          return get8(Y + (int64_t)(i0 + m) * w.mp + j0 + n, px);
         },
         [&](int m, int n, float (&v)[8], const auto& x) __attribute__((always_inline)) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] = fmaf(a.a, value(x, e), back * v[e]);
-          put<PLANES>(out + (int64_t)(i0 + m) * w.mp + j0 + n, px, v);
+          put(out + (int64_t)(i0 + m) * w.mp + j0 + n, px, v);
         },
         [](int, int, const float (&)[8]) {}, false);
   } else {
@@ -263,7 +258,7 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch
     product_rows_cols<8>(
         sums, smem,
         [&](int m, int n) __attribute__((always_inline)) {
-          return get8<PLANES>(Y + (int64_t)(i0 + m) * w.mp + j0 + n, px);
+          return get8(Y + (int64_t)(i0 + m) * w.mp + j0 + n, px);
         },
         [&](int m, int n, float (&v)[8], const auto& x) __attribute__((always_inline)) {
           const int i = i0 + m, j = j0 + n;
@@ -288,13 +283,12 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch
 __device__ __forceinline__ int lds_swizzle(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
 
 // Eight k of each of 32 rows from r0 on: step ks of 16.
-template <int PLANES>
-__device__ __forceinline__ Parts8<PLANES> lds_fragment(const unsigned char* M, int pitch, int plane,
+__device__ __forceinline__ Parts8 lds_fragment(const unsigned char* M, int pitch, int plane,
                                                        int r0, int ks) {
   const int lane = threadIdx.x & 63, r = r0 + (lane & 31);
-  Parts8<PLANES> f;
+  Parts8 f;
 #pragma unroll
-  for (int p = 0; p < PLANES; ++p)
+  for (int p = 0; p < kParts; ++p)
     f.p[p] = *reinterpret_cast<const u32x4*>(M + p * plane + r * pitch +
                                              (((2 * ks + (lane >> 5)) ^ lds_swizzle(r)) * 16));
   return f;
@@ -302,16 +296,12 @@ __device__ __forceinline__ Parts8<PLANES> lds_fragment(const unsigned char* M, i
 // All products of the parts, lo lo too: the diagonal of A sums squares, so what is left
 // out has one sign, which shows with few singular values (fp32, 16 x 100, 4 draws: mean
 // error 1.3e-6, with lo lo 1.0e-6).
-template <int PLANES>
-__device__ __forceinline__ void multiply_parts(const Parts8<PLANES>& b, const Parts8<PLANES>& l,
+__device__ __forceinline__ void multiply_parts(const Parts8& b, const Parts8& l,
                                                f32x16& acc) {
-  constexpr int MODE = PLANES == 2 ? kF16x2 : kF16;
-  if constexpr (PLANES == 2) {
-    acc = product_mfma<MODE>(b.p[PLANES - 1], l.p[PLANES - 1], acc);
-    acc = product_mfma<MODE>(b.p[PLANES - 1], l.p[0], acc);
-    acc = product_mfma<MODE>(b.p[0], l.p[PLANES - 1], acc);
-  }
-  acc = product_mfma<MODE>(b.p[0], l.p[0], acc);
+  acc = product_mfma<kF16x2>(b.p[1], l.p[1], acc);
+  acc = product_mfma<kF16x2>(b.p[1], l.p[0], acc);
+  acc = product_mfma<kF16x2>(b.p[0], l.p[1], acc);
+  acc = product_mfma<kF16x2>(b.p[0], l.p[0], acc);
 }
 
 // ---- medium matrices: A's square and its product with Y in one launch -------------------
@@ -325,26 +315,26 @@ __device__ __forceinline__ void multiply_parts(const Parts8<PLANES>& b, const Pa
 // compile-time constant: at run time its divisions alone took 3 us.
 constexpr int kBandWaves = 8, kBandRows = 32;
 
-template <int PLANES, int mp>
+template <int mp>
 __global__ __launch_bounds__(64 * kBandWaves) void newton_band_kernel(NewtonLaunch a, NewtonWork w,
                                                                       int from) {
   constexpr int THREADS = 64 * kBandWaves, slots = mp / 8, pitch = mp * 2;
   constexpr int plane_a = mp * pitch, plane_y = kBandRows * pitch;
-  __shared__ __attribute__((aligned(16))) unsigned char smem[PLANES * (plane_a + plane_y)];
+  __shared__ __attribute__((aligned(16))) unsigned char smem[kParts * (plane_a + plane_y)];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int bands = w.np / kBandRows, id = xcd_tile(blockIdx.x, gridDim.x);
   const int64_t z = id / bands, i0 = (int64_t)(id % bands) * kBandRows;
   const int64_t px = (int64_t)mp * w.np, pa = (int64_t)mp * mp;
-  const uint16_t* const Y = w.Y[from] + z * PLANES * px + i0 * mp;
-  uint16_t* const out = w.Y[1 - from] + z * PLANES * px + i0 * mp;
-  const uint16_t* const A = w.A + z * PLANES * pa;
+  const uint16_t* const Y = w.Y[from] + z * kParts * px + i0 * mp;
+  uint16_t* const out = w.Y[1 - from] + z * kParts * px + i0 * mp;
+  const uint16_t* const A = w.A + z * kParts * pa;
   unsigned char* const lds_a = smem;                          // planes of mp rows
-  unsigned char* const lds_y = smem + PLANES * plane_a;       // planes of 32 rows
+  unsigned char* const lds_y = smem + kParts * plane_a;       // planes of 32 rows
   auto at = [&](unsigned char* M, int r, int slot) __attribute__((always_inline)) {
     return reinterpret_cast<u32x4*>(M + r * pitch + ((slot ^ lds_swizzle(r)) * 16));
   };
-  constexpr int VECTORS = PLANES * mp * slots, BATCH = (VECTORS + THREADS - 1) / THREADS;
+  constexpr int VECTORS = kParts * mp * slots, BATCH = (VECTORS + THREADS - 1) / THREADS;
   u32x4 v[BATCH];  // all of a thread's loads in flight
 #pragma unroll
   for (int u = 0; u < BATCH; ++u) {
@@ -357,7 +347,7 @@ __global__ __launch_bounds__(64 * kBandWaves) void newton_band_kernel(NewtonLaun
     if (VECTORS % THREADS == 0 || q < VECTORS)
       *at(lds_a + row / mp * plane_a, row % mp, q % slots) = v[u];
   }
-  for (int q = tid; q < PLANES * kBandRows * slots; q += THREADS) {
+  for (int q = tid; q < kParts * kBandRows * slots; q += THREADS) {
     const int p = q / (kBandRows * slots), e = q % (kBandRows * slots);
     *at(lds_y + p * plane_y, e / slots, e % slots) =
         *reinterpret_cast<const u32x4*>(Y + p * px + e * 8);
@@ -373,8 +363,8 @@ __global__ __launch_bounds__(64 * kBandWaves) void newton_band_kernel(NewtonLaun
     clear_block(acc);
 #pragma unroll
     for (int ks = 0; ks < mp / 16; ++ks)
-      multiply_parts<PLANES>(lds_fragment<PLANES>(lds_a, pitch, plane_a, 32 * wave, ks),
-                             lds_fragment<PLANES>(lds_y, pitch, plane_y, 0, ks), acc);
+      multiply_parts(lds_fragment(lds_a, pitch, plane_a, 32 * wave, ks),
+                             lds_fragment(lds_y, pitch, plane_y, 0, ks), acc);
   };
   // The lane's columns 8 g + 4 (lane / 32) of the wave's, row i of the band.
   auto place = [&](int g) __attribute__((always_inline)) {
@@ -388,12 +378,11 @@ __global__ __launch_bounds__(64 * kBandWaves) void newton_band_kernel(NewtonLaun
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const uint2 hi = *reinterpret_cast<const uint2*>(place(g));
-      uint2 lo = make_uint2(0, 0);
-      if constexpr (PLANES == 2) lo = *reinterpret_cast<const uint2*>(place(g) + plane_y / 2);
+      const uint2 lo = *reinterpret_cast<const uint2*>(place(g) + plane_y / 2);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float y = unpack_f16(e < 2 ? hi.x : hi.y, e & 1);
-        if constexpr (PLANES == 2) y += unpack_f16(e < 2 ? lo.x : lo.y, e & 1);
+        const float y =
+            unpack_f16(e < 2 ? hi.x : hi.y, e & 1) + unpack_f16(e < 2 ? lo.x : lo.y, e & 1);
         sum[4 * g + e] = fmaf(a.a, y, a.b * back * acc[4 * g + e]);
       }
     }
@@ -405,7 +394,7 @@ __global__ __launch_bounds__(64 * kBandWaves) void newton_band_kernel(NewtonLaun
       float t[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) t[e] = back * acc[4 * g + e];
-      put<PLANES>(place(g), plane_y / 2, t);
+      put(place(g), plane_y / 2, t);
     }
   __syncthreads();
   if (works) product();
@@ -416,10 +405,10 @@ __global__ __launch_bounds__(64 * kBandWaves) void newton_band_kernel(NewtonLaun
       float y[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] = fmaf(a.c * back, acc[4 * g + e], sum[4 * g + e]);
-      put<PLANES>(place(g), plane_y / 2, y);
+      put(place(g), plane_y / 2, y);
     }
   __syncthreads();
-  for (int q = tid; q < PLANES * kBandRows * slots; q += THREADS) {
+  for (int q = tid; q < kParts * kBandRows * slots; q += THREADS) {
     const int p = q / (kBandRows * slots), e = q % (kBandRows * slots);
     *reinterpret_cast<u32x4*>(out + p * px + e * 8) =
         *at(lds_y + p * plane_y, e / slots, e % slots);
@@ -446,7 +435,7 @@ inline bool fits_one_block(const NewtonWork& w) {
 template <bool BF16>
 __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLaunch a,
                                                                         NewtonWork w) {
-  constexpr int PLANES = 2, THREADS = 64 * kSmallWaves;
+  constexpr int THREADS = 64 * kSmallWaves;
   __shared__ __attribute__((aligned(16))) unsigned char smem[kSmallLds];
   __shared__ double norms[kSmallWaves];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -454,7 +443,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
   const int mp = w.mp, np = w.np, mb = mp / 32, nb = np / 32;
   const int64_t size = (int64_t)a.rows * a.cols, base = blockIdx.x * size;
   unsigned char* const X = smem;                          // planes of mp rows of np
-  unsigned char* const A = smem + PLANES * mp * np * 2;   // planes of mp rows of mp
+  unsigned char* const A = smem + kParts * mp * np * 2;   // planes of mp rows of mp
   const int px = mp * np * 2, pa = mp * mp * 2;
 
   // The norm, with the momentum's update.
@@ -482,7 +471,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
   for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o);
   if (lane == 0) norms[wave] = s;
   // X's padding.
-  for (int q = tid; q < PLANES * mp * np / 8; q += THREADS)
+  for (int q = tid; q < kParts * mp * np / 8; q += THREADS)
     reinterpret_cast<u32x4*>(X)[q] = u32x4{0, 0, 0, 0};
   __syncthreads();
   s = 0.0;
@@ -503,7 +492,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
       const float v = (float)(u[e] * inv);
       const _Float16 hi = (_Float16)v;
       *reinterpret_cast<_Float16*>(to) = hi;
-      if constexpr (PLANES == 2) *reinterpret_cast<_Float16*>(to + px) = (_Float16)(v - (float)hi);
+      *reinterpret_cast<_Float16*>(to + px) = (_Float16)(v - (float)hi);
     }
   }
   __syncthreads();
@@ -511,10 +500,10 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
   const int frag_row = lane & 31, half = lane >> 5;
   // Columns c0 .. c0 + 31 of X, k along its rows.
   auto col_frag = [&](int c0, int ks) __attribute__((always_inline)) {
-    Parts8<PLANES> f;
+    Parts8 f;
     const int c = c0 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
 #pragma unroll
-    for (int p = 0; p < PLANES; ++p)
+    for (int p = 0; p < kParts; ++p)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int k = 16 * ks + 8 * half + 4 * h + ((lane >> 2) & 3);
@@ -543,17 +532,15 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
         for (int e = 0; e < 4; ++e) v[e] = q * sum[4 * g + e];
       } else {
         const uint2 hi = *reinterpret_cast<const uint2*>(at);
-        uint2 lo = make_uint2(0, 0);
-        if constexpr (PLANES == 2) lo = *reinterpret_cast<const uint2*>(at + plane / 2);
+        const uint2 lo = *reinterpret_cast<const uint2*>(at + plane / 2);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const uint32_t h = e < 2 ? hi.x : hi.y, l = e < 2 ? lo.x : lo.y;
-          float old = unpack_f16(h, e & 1);
-          if constexpr (PLANES == 2) old += unpack_f16(l, e & 1);
+          const float old = unpack_f16(h, e & 1) + unpack_f16(l, e & 1);
           v[e] = fmaf(p, old, q * sum[4 * g + e]);
         }
       }
-      put<PLANES>(at, plane / 2, v);
+      put(at, plane / 2, v);
     }
   };
   const float back = 1.0f / kScale;  // products carry the scale twice
@@ -565,7 +552,8 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
       const int bi = b / mb, bj = b % mb;
       clear_block(acc[0]);
       for (int ks = 0; ks < np / 16; ++ks)
-        multiply_parts<PLANES>(lds_fragment<PLANES>(X, np * 2, px, 32 * bj, ks), lds_fragment<PLANES>(X, np * 2, px, 32 * bi, ks), acc[0]);
+        multiply_parts(lds_fragment(X, np * 2, px, 32 * bj, ks),
+                       lds_fragment(X, np * 2, px, 32 * bi, ks), acc[0]);
       update(A, mp * 2, pa, bi, bj, 0.0f, back, acc[0]);
     }
     __syncthreads();
@@ -577,8 +565,8 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
       for (int t = 0; t < kSmallBlocks; ++t) {
         const int b = wave + t * kSmallWaves;
         if (b < mb * mb)
-          multiply_parts<PLANES>(lds_fragment<PLANES>(A, mp * 2, pa, 32 * (b % mb), ks),
-                   lds_fragment<PLANES>(A, mp * 2, pa, 32 * (b / mb), ks), acc[t]);
+          multiply_parts(lds_fragment(A, mp * 2, pa, 32 * (b % mb), ks),
+                         lds_fragment(A, mp * 2, pa, 32 * (b / mb), ks), acc[t]);
       }
     __syncthreads();
 #pragma unroll
@@ -595,7 +583,8 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
       for (int t = 0; t < kSmallBlocks; ++t) {
         const int b = wave + t * kSmallWaves;
         if (b < mb * nb)
-          multiply_parts<PLANES>(col_frag(32 * (b / mb), ks), lds_fragment<PLANES>(A, mp * 2, pa, 32 * (b % mb), ks), acc[t]);
+          multiply_parts(col_frag(32 * (b / mb), ks),
+                         lds_fragment(A, mp * 2, pa, 32 * (b % mb), ks), acc[t]);
       }
     __syncthreads();
 #pragma unroll
@@ -619,8 +608,8 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
       if (e < cols) {
         const unsigned char* const from =
             X + i * np * 2 + (((j >> 3) ^ lds_swizzle(i)) * 16) + (j & 7) * 2;
-        v[e] = (float)*reinterpret_cast<const _Float16*>(from);
-        if constexpr (PLANES == 2) v[e] += (float)*reinterpret_cast<const _Float16*>(from + px);
+        v[e] = (float)*reinterpret_cast<const _Float16*>(from) +
+               (float)*reinterpret_cast<const _Float16*>(from + px);
       }
       v[e] *= back;
       if (a.weight) v[e] = fmaf(a.decay, old[e], -a.rate * v[e]);
@@ -641,7 +630,7 @@ inline int64_t tiles_of(const NewtonWork& w, int64_t batch, bool symmetric, int 
   return (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batch;
 }
 inline bool small_tiles(const NewtonWork& w, int64_t batch, bool symmetric) {
-  return tiles_of(w, batch, symmetric, 64) <= (w.two ? 1024 : 768);
+  return tiles_of(w, batch, symmetric, 64) <= 1024;
 }
 
 template <class C, int KIND, bool BF16>
@@ -651,36 +640,24 @@ void launch_one(const NewtonLaunch& a, const NewtonWork& w, int from, hipStream_
                      dim3(C::THREADS), 0, s, a, w, from, (int)tiles);
 }
 
-template <int KIND, bool BF16, int PLANES>
+template <int KIND, bool BF16>
 void launch_product(const NewtonLaunch& a, const NewtonWork& w, int from, hipStream_t s) {
   constexpr bool kSymmetric = KIND == kGram || KIND == kSquare, kCol = KIND == kGram;
   const bool small = small_tiles(w, a.batch, kSymmetric);
-  if constexpr (PLANES == 1) {
-    if (small && tiles_of(w, a.batch, kSymmetric, 64) <= 512)
-      launch_one<RingCfg<kF16, 64, 64, 64, 2, 2, kCol, kCol, 4>, KIND, BF16>(a, w, from, s);
-    else if (small)
-      launch_one<RingCfg<kF16, 64, 64, 64, 2, 2, kCol, kCol, 2>, KIND, BF16>(a, w, from, s);
-    else if (tiles_of(w, a.batch, kSymmetric, 128) <= 256)
-      launch_one<RingCfg<kF16, 128, 128, 64, 2, 2, kCol, kCol, 4>, KIND, BF16>(a, w, from, s);
-    else
-      launch_one<RingCfg<kF16, 128, 128, 64, 2, 2, kCol, kCol, 2, 1, 1>, KIND, BF16>(a, w, from, s);
-  } else {
-    if (small && tiles_of(w, a.batch, kSymmetric, 64) <= 256)
-      launch_one<RingCfg<kF16x2, 64, 64, 64, 2, 2, kCol, kCol, 4>, KIND, BF16>(a, w, from, s);
-    else if (small)
-      launch_one<RingCfg<kF16x2, 64, 64, 64, 2, 2, kCol, kCol, 2>, KIND, BF16>(a, w, from, s);
-    else
-      launch_one<RingCfg<kF16x2, 128, 128, 32, 2, 2, kCol, kCol, 4>, KIND, BF16>(a, w, from, s);
-  }
+  if (small && tiles_of(w, a.batch, kSymmetric, 64) <= 256)
+    launch_one<RingCfg<kF16x2, 64, 64, 64, 2, 2, kCol, kCol, 4>, KIND, BF16>(a, w, from, s);
+  else if (small)
+    launch_one<RingCfg<kF16x2, 64, 64, 64, 2, 2, kCol, kCol, 2>, KIND, BF16>(a, w, from, s);
+  else
+    launch_one<RingCfg<kF16x2, 128, 128, 32, 2, 2, kCol, kCol, 4>, KIND, BF16>(a, w, from, s);
 }
 
 inline size_t aligned(size_t v) { return (v + 255) / 256 * 256; }
 
-size_t layout(int64_t batch, int rows, int cols, bool bf16, unsigned char* ws, NewtonWork* w) {
+size_t layout(int64_t batch, int rows, int cols, unsigned char* ws, NewtonWork* w) {
   w->flip = rows > cols;
   w->m = w->flip ? cols : rows;
   w->n = w->flip ? rows : cols;
-  w->two = !bf16 || w->m <= 64;
   w->mp = (w->m + 63) / 64 * 64;
   w->np = (w->n + 63) / 64 * 64;
   if (!small_tiles(*w, batch, true) || !small_tiles(*w, batch, false)) {
@@ -689,9 +666,8 @@ size_t layout(int64_t batch, int rows, int cols, bool bf16, unsigned char* ws, N
   }
   const int64_t blocks = ((int64_t)rows * cols + 4095) / 4096;
   w->norm_blocks = (int)(blocks < kMaxNormBlocks ? blocks : kMaxNormBlocks);
-  const size_t planes = w->two ? 2 : 1;
-  const size_t x = aligned((size_t)batch * planes * w->mp * w->np * 2);
-  const size_t g = aligned((size_t)batch * planes * w->mp * w->mp * 2);
+  const size_t x = aligned((size_t)batch * kParts * w->mp * w->np * 2);
+  const size_t g = aligned((size_t)batch * kParts * w->mp * w->mp * 2);
   const size_t norms = aligned((size_t)batch * kMaxNormBlocks * sizeof(double));
   w->norms = reinterpret_cast<double*>(ws);
   uint16_t* const rest = reinterpret_cast<uint16_t*>(ws + norms);
@@ -712,25 +688,20 @@ bool one_block(NewtonWork* w) {
   return true;
 }
 
-template <int PLANES, int MP>
+template <int MP>
 bool launch_band_of(const NewtonLaunch& a, const NewtonWork& w, int from, hipStream_t s) {
   if (w.mp != MP) return false;
-  hipLaunchKernelGGL((newton_band_kernel<PLANES, MP>),
+  hipLaunchKernelGGL((newton_band_kernel<MP>),
                      dim3((unsigned)(w.np / kBandRows * a.batch)), dim3(64 * kBandWaves), 0, s, a, w,
                      from);
   return true;
 }
-template <int PLANES>
 bool launch_band(const NewtonLaunch& a, const NewtonWork& w, int from, hipStream_t s) {
-  if constexpr (PLANES == 1)
-    return launch_band_of<1, 128>(a, w, from, s) || launch_band_of<1, 192>(a, w, from, s) ||
-           launch_band_of<1, 256>(a, w, from, s);
-  else
-    return launch_band_of<2, 64>(a, w, from, s) || launch_band_of<2, 128>(a, w, from, s);
+  return launch_band_of<64>(a, w, from, s) || launch_band_of<128>(a, w, from, s);
 }
 
-template <bool BF16, int PLANES>
-hipError_t launch_parts(const NewtonLaunch& a, NewtonWork w, hipStream_t s) {
+template <bool BF16>
+hipError_t launch_dtype(const NewtonLaunch& a, NewtonWork w, hipStream_t s) {
   const unsigned batch = (unsigned)a.batch;
   if (one_block(&w)) {
     hipLaunchKernelGGL(newton_small_kernel<BF16>, dim3(batch), dim3(64 * kSmallWaves), 0, s, a, w);
@@ -738,32 +709,31 @@ hipError_t launch_parts(const NewtonLaunch& a, NewtonWork w, hipStream_t s) {
   }
   hipLaunchKernelGGL(newton_norm_kernel<BF16>, dim3((unsigned)w.norm_blocks, batch), dim3(256), 0, s,
                      a, w);
-  hipLaunchKernelGGL((newton_start_kernel<BF16, PLANES>),
+  hipLaunchKernelGGL(newton_start_kernel<BF16>,
                      dim3((unsigned)(w.mp / 64), (unsigned)(w.np / 64), batch), dim3(256), 0, s, a, w);
   for (int k = 0, from = 0; k < a.steps; ++k, from = 1 - from) {
-    launch_product<kGram, BF16, PLANES>(a, w, from, s);
-    if (k + 1 < a.steps && launch_band<PLANES>(a, w, from, s)) continue;
-    launch_product<kSquare, BF16, PLANES>(a, w, from, s);
-    if (k + 1 < a.steps) launch_product<kApply, BF16, PLANES>(a, w, from, s);
-    else launch_product<kLast, BF16, PLANES>(a, w, from, s);
+    launch_product<kGram, BF16>(a, w, from, s);
+    if (k + 1 < a.steps && launch_band(a, w, from, s)) continue;
+    launch_product<kSquare, BF16>(a, w, from, s);
+    if (k + 1 < a.steps) launch_product<kApply, BF16>(a, w, from, s);
+    else launch_product<kLast, BF16>(a, w, from, s);
   }
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t newton_workspace(int64_t batch, int rows, int cols, bool bf16) {
+size_t newton_workspace(int64_t batch, int rows, int cols) {
   NewtonWork w;
-  return layout(batch, rows, cols, bf16, nullptr, &w);
+  return layout(batch, rows, cols, nullptr, &w);
 }
 
 hipError_t launch_newton(const NewtonLaunch& a, void* workspace, hipStream_t s) {
   if (a.batch <= 0) return hipSuccess;
   ProfileScope prof(kKNewtonSchulz, s);
   NewtonWork w;
-  layout(a.batch, a.rows, a.cols, a.bf16, static_cast<unsigned char*>(workspace), &w);
-  if (!a.bf16) return launch_parts<false, 2>(a, w, s);
-  return w.two ? launch_parts<true, 2>(a, w, s) : launch_parts<true, 1>(a, w, s);
+  layout(a.batch, a.rows, a.cols, static_cast<unsigned char*>(workspace), &w);
+  return a.bf16 ? launch_dtype<true>(a, w, s) : launch_dtype<false>(a, w, s);
 }
 
 }  // namespace pinsage

@@ -7,7 +7,6 @@
 //
 // Modes:
 //   kBf16   bf16 in memory, one MFMA per product
-//   kF16    fp16 in memory, the same
 //   kF16x2  two fp16 parts in memory (x = hi + lo, planes apart by `plane`
 //           bytes): 22 significand bits, three MFMAs (hi lo, lo hi, hi hi); for
 //           operands the caller keeps inside fp16's range
@@ -29,7 +28,7 @@ namespace pinsage {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-enum ProductMode { kBf16 = 0, kF16 = 1, kF16x2 = 2, kF32 = 3 };
+enum ProductMode { kBf16 = 0, kF16x2 = 2, kF32 = 3 };
 
 // A tile's operand: `p` at the tile's first row (row operand, k = 0) or first
 // column (column operand, k = 0); `valid` rows exist from there (at least 1).
@@ -132,7 +131,7 @@ __device__ __forceinline__ int product_swizzle(int row) {
 
 template <int MODE>
 __device__ __forceinline__ f32x16 product_mfma(const u32x4& b, const u32x4& a, const f32x16& c) {
-  if constexpr (MODE == kF16 || MODE == kF16x2)
+  if constexpr (MODE == kF16x2)
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, b),
                                                   __builtin_bit_cast(f16x8, a), c, 0, 0, 0);
   else
