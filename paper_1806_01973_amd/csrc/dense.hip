@@ -675,8 +675,10 @@ __global__ __launch_bounds__(64 * kJoinWaves) void dense_join_kernel(DenseGradLa
 }
 
 // ---- tile shapes -----------------------------------------------------------------
-// Ring: rows of whole 16-byte vectors; else through registers, which 256 x 256 leaves
-// none of.
+// Ring: rows of whole 16-byte vectors; else through registers, of which 256 x 256
+// leaves none, nor 128 x 128 in fp32 (by 64 and by 128 x 64, the largest without scratch:
+// 120,011 rows of 255 -> 257 224 us, 215, gradients 655, 724; 60,003 of 511 -> 259 217,
+// 206 and 589, 570).
 template <bool BF16, bool A_COL, bool B_COL>
 struct Tiles;
 template <bool A_COL, bool B_COL>
@@ -694,8 +696,8 @@ struct Tiles<false, A_COL, B_COL> {
   using RingSmall = RingCfg<kF32, 64, 64, 16, 2, 2, A_COL, B_COL, 4>;
   using RingMany = RingSmall;
   using RingBig = RingMid;
-  using Mid = RingCfg<kF32, 128, 128, 16, 2, 2, A_COL, B_COL, 2, 2, 0, true>;
   using Small = RingCfg<kF32, 64, 64, 32, 2, 2, A_COL, B_COL, 2, 3, 0, true>;
+  using Mid = Small;
 };
 
 enum Shape { kSmall, kMid, kBig };

@@ -11,11 +11,12 @@
 //           bytes): 22 significand bits, three MFMAs (hi lo, lo hi, hi hi); for
 //           operands the caller keeps inside fp16's range
 //   kF32    fp32 in memory, split on the way to the MFMAs into three bf16 parts (24
-//           significand bits), six MFMAs: all products of parts down to 2^-17 of
-//           the leading one. Left out is at most 2^-25 of a product, as fp32's own
-//           rounding. Infinities and NaN, and values that round to a bf16
-//           infinity, make an element that is not finite; the caller takes such
-//           elements from redo_not_finite.
+//           significand bits), eight MFMAs, the leading products in sums of their
+//           own: what is left out is below 2^-33 of a product (split_device.h).
+//           Elements of rows and columns that the parts do not cover come from fp32
+//           MFMAs. Infinities and NaN, and values that round to a bf16 infinity,
+//           make an element that is not finite; the caller takes such elements from
+//           redo_not_finite.
 // Sums run in fp32, chunks in order, so an element's bits follow from its row,
 // its column and the k range alone, whatever tile it lies in.
 #pragma once

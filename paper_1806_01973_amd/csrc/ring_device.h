@@ -17,7 +17,9 @@
 // s ^ ring_col_swizzle(k); of fp32 as eight 4-byte reads.
 // fp32 values are split into their three bf16 parts after the LDS read, among the
 // MFMAs of the step before: 7 VALU instructions a value, twice per value and tile
-// with 64 x 64 wave tiles, under 6 MFMAs per product.
+// with 64 x 64 wave tiles, under 8 MFMAs per product, and the least magnitudes are
+// kept. A tile of which the parts do not cover some pair of rows (split_covers) is
+// formed again with fp32 MFMAs.
 //
 // What bounds large products are the MFMAs, in 63% of the cycles of 8,192 cubed by
 // 256 x 256 (counted when it took 943 us; it takes 878), and the clock, which power holds
@@ -62,12 +64,15 @@ struct RingCfg {
   static constexpr int STAGE_LD = WN + 4;
   static constexpr int STAGE_BYTES = 32 * STAGE_LD * 4;
   static constexpr int RING = (STAGES + AHEAD) * A_BYTES + STAGES * B_BYTES;
-  static constexpr int LDS_BYTES = RING > NWAVES * STAGE_BYTES ? RING : NWAVES * STAGE_BYTES;
+  // kF32: behind the ring a word a wave, whether it wants the tile again.
+  static constexpr int FLAGS = RING > NWAVES * STAGE_BYTES ? RING : NWAVES * STAGE_BYTES;
+  static constexpr int LDS_BYTES = FLAGS + (MODE == kF32 ? 4 * NWAVES : 0);
   static_assert(A_GROUPS * MEM_PLANES % NWAVES == 0 && B_GROUPS * MEM_PLANES % NWAVES == 0 &&
                     A_GROUPS % DA == 0 && B_GROUPS % DB == 0,
                 "every wave serves one plane of each operand");
   static_assert(STAGES >= 2 && PENDING <= 63 && LDS_BYTES <= 160 * 1024, "");
   static_assert(!REGS || (MEM_PLANES == 1 && AHEAD == 0), "");
+  static_assert(MODE != kF32 || AHEAD == 0, "");
   static_assert(BK * ESZ == 64 || BK * ESZ == 128, "rows of 4 or 8 slots");
 };
 
@@ -138,6 +143,13 @@ __device__ __forceinline__ void tile_sums(const Operand& A, const Operand& B, in
   for (int i = 0; i < C::TM; ++i)
 #pragma unroll
     for (int j = 0; j < C::TN; ++j) clear_block(acc[i][j]);
+  // kF32: the sums of the products of parts beside the leading one.
+  f32x16 small[C::MODE == kF32 ? C::TM : 1][C::TN];
+  if constexpr (C::MODE == kF32)
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < C::TN; ++j) clear_block(small[i][j]);
   const int nchunks = __builtin_amdgcn_readfirstlane((int)((k1 - k0 + BK - 1) / BK));
   if (nchunks <= 0) return;
   const uint32_t smem_base =
@@ -177,6 +189,8 @@ __device__ __forceinline__ void tile_sums(const Operand& A, const Operand& B, in
   const int64_t step_b = (C::B_COL ? B.ld * BK : BK) * ESZ;
   base_a = ring_uniform(base_a + (C::A_COL ? k0 * A.ld : k0) * ESZ);
   base_b = ring_uniform(base_b + (C::B_COL ? k0 * B.ld : k0) * ESZ);
+  const unsigned char* const first_base_a = base_a;
+  const unsigned char* const first_base_b = base_b;
   const int whole = __builtin_amdgcn_readfirstlane((int)((k1 - k0) / BK));  // chunks inside k
   const int rest = (int)((k1 - k0) % BK);
   // DMA d of a turn: B's of chunk `turn` and A's of chunk turn + AHEAD, in this order.
@@ -338,18 +352,19 @@ __device__ __forceinline__ void tile_sums(const Operand& A, const Operand& B, in
   auto read = [&](int c, int ks, Frags& f) __attribute__((always_inline)) {
     unroll<0, FRAGS>([&](auto q) __attribute__((always_inline)) { read_one(c, ks, f, q); });
   };
+  // kF32: the least magnitudes of the values this lane has split.
+  uint32_t key_a = ~0u, key_b = ~0u;
   auto split = [&](Frags& f) __attribute__((always_inline)) {
     if constexpr (ESZ == 4) {
-      uint32_t key = 0;
 #pragma unroll
       for (int i = 0; i < C::TM; ++i) {
-        const Split3 s = split3(f.a[i][0], f.a[i][1], key);
+        const Split3 s = split3(f.a[i][0], f.a[i][1], key_a);
 #pragma unroll
         for (int p = 0; p < 3; ++p) f.a[i][p] = s.p[p];
       }
 #pragma unroll
       for (int j = 0; j < C::TN; ++j) {
-        const Split3 s = split3(f.b[j][0], f.b[j][1], key);
+        const Split3 s = split3(f.b[j][0], f.b[j][1], key_b);
 #pragma unroll
         for (int p = 0; p < 3; ++p) f.b[j][p] = s.p[p];
       }
@@ -362,7 +377,8 @@ __device__ __forceinline__ void tile_sums(const Operand& A, const Operand& B, in
   // cubed by 256 x 256: 1,005 us, the DMAs spread 979; with A a stage ahead 900, the
   // reads spread too 878. By 64 x 64, one MFMA a step, it loses: 1,024 x 1,024 x 2,048
   // 11.0 us, spread 15.0).
-  constexpr int PRODUCTS = PARTS * (PARTS + 1) / 2, ALL = PRODUCTS * C::TM * C::TN;
+  constexpr int PRODUCTS = PARTS == 3 ? kSplitProducts : (PARTS == 2 ? 3 : 1);
+  constexpr int ALL = PRODUCTS * C::TM * C::TN;
   constexpr bool kSpread = ESZ == 2 && ALL >= 4;
   auto work = [&](const Frags& cur, Frags& nxt, int c, int ks, int turn, auto from, auto to)
       __attribute__((always_inline)) {
@@ -377,9 +393,9 @@ __device__ __forceinline__ void tile_sums(const Operand& A, const Operand& B, in
     unroll<0, ALL>([&](auto at) __attribute__((always_inline)) {
       constexpr int e = decltype(at)::value, q = e / (C::TM * C::TN), i = e / C::TN % C::TM,
                     j = e % C::TN;
-      constexpr int kB3[6] = {2, 0, 1, 1, 0, 0}, kA3[6] = {0, 2, 1, 0, 1, 0};
-      constexpr int pb = kB3[6 - PRODUCTS + q], pa = kA3[6 - PRODUCTS + q];
-      acc[i][j] = product_mfma<C::MODE>(cur.b[j][pb], cur.a[i][pa], acc[i][j]);
+      constexpr int t = kSplitProducts - PRODUCTS + q, pb = split_b(t), pa = split_a(t);
+      f32x16& sum = C::MODE == kF32 && q < PRODUCTS - 1 ? small[C::MODE == kF32 ? i : 0][j] : acc[i][j];
+      sum = product_mfma<C::MODE>(cur.b[j][pb], cur.a[i][pa], sum);
       if constexpr (kSpread) {
         constexpr int r0 = (e * FRAGS + ALL - 1) / ALL, r1 = ((e + 1) * FRAGS + ALL - 1) / ALL;
         constexpr int d0 = e * DMAS / ALL, d1 = (e + 1) * DMAS / ALL;
@@ -439,10 +455,15 @@ __device__ __forceinline__ void tile_sums(const Operand& A, const Operand& B, in
     });
     if constexpr (!C::REGS) ring_wait<C::PENDING>();
     ring_barrier();
-    // Past the last chunk what is read is not used.
+    // Past the last chunk what is read is not used (zeros, with REGS anything).
     Frags &cur = f[(P + C::STEPS - 1) & 1], &nxt = f[(P + C::STEPS) & 1];
     if constexpr (C::REGS) {
+      const uint32_t had_a = key_a, had_b = key_b;
       work(cur, nxt, c + 1, 0, 0, None{}, None{});
+      if (c + 1 >= nchunks) {
+        key_a = had_a;
+        key_b = had_b;
+      }
       store(c + STAGES, held);
       fetch(c + STAGES + 1, held);
     } else {
@@ -464,7 +485,92 @@ __device__ __forceinline__ void tile_sums(const Operand& A, const Operand& B, in
     for (; c < nchunks; ++c) chunk(c, Even{});
   }
   if constexpr (!C::REGS) ring_wait<0>();
+  bool covered = true;
+  if constexpr (C::MODE == kF32) {
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < C::TN; ++j) acc[i][j] += small[i][j];
+    covered = split_covers(wave_min_key(key_a), wave_min_key(key_b));
+    if (lane == 0) reinterpret_cast<uint32_t*>(smem + C::FLAGS)[wave] = !covered;
+  }
   __syncthreads();
+  if constexpr (C::MODE == kF32) {
+    uint32_t again = 0;
+#pragma unroll
+    for (int w = 0; w < C::NWAVES; ++w) again |= reinterpret_cast<const uint32_t*>(smem + C::FLAGS)[w];
+    if (again) {
+      // The tile again with fp32 MFMAs (operand q of a step pairs half-wave h with its
+      // column 8 h + q), a chunk in flight. Each element then follows from its own row
+      // and column alone: split where those are covered, else fp32, so that it does not
+      // depend on the tile it lies in.
+      f32x16 full[C::TM][C::TN];
+      uint32_t least_a[C::TM], least_b[C::TN];
+#pragma unroll
+      for (int i = 0; i < C::TM; ++i) least_a[i] = ~0u;
+#pragma unroll
+      for (int j = 0; j < C::TN; ++j) least_b[j] = ~0u;
+#pragma unroll
+      for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j) clear_block(full[i][j]);
+      base_a = first_base_a;
+      base_b = first_base_b;
+      if constexpr (C::REGS) fetch(0, held);
+      else issue(0, None{}, Every{});
+#pragma unroll 1
+      for (int c = 0; c < nchunks; ++c) {
+        if constexpr (C::REGS) {
+          store(c, held);
+          fetch(c + 1, held);
+          ring_barrier();
+        } else {
+          ring_wait<0>();
+          ring_barrier();
+          if (c + 1 < nchunks) issue(c + 1, None{}, Every{});
+        }
+        if (covered) continue;  // the wave only loads
+#pragma unroll
+        for (int ks = 0; ks < C::STEPS; ++ks) {
+          read(c, ks, f[0]);
+#pragma unroll
+          for (int i = 0; i < C::TM; ++i)
+            least_a[i] = least_key(f[0].a[i][0], f[0].a[i][1], least_a[i]);
+#pragma unroll
+          for (int j = 0; j < C::TN; ++j)
+            least_b[j] = least_key(f[0].b[j][0], f[0].b[j][1], least_b[j]);
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+              for (int j = 0; j < C::TN; ++j)
+                full[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(
+                    __uint_as_float(f[0].b[j][q >> 2][q & 3]),
+                    __uint_as_float(f[0].a[i][q >> 2][q & 3]), full[i][j], 0, 0, 0);
+        }
+      }
+      if (!covered) {
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+          least_a[i] = umin(least_a[i], (uint32_t)__shfl_xor((int)least_a[i], 32));
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j) {
+          least_b[j] = umin(least_b[j], (uint32_t)__shfl_xor((int)least_b[j], 32));
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            // A lane's row of block i; its element e's column is this lane's of the fragment.
+            const uint32_t kb =
+                (uint32_t)__shfl((int)least_b[j], 8 * (e >> 2) + 4 * half + (e & 3));
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i)
+              acc[i][j][e] = split_covers(least_a[i], kb) ? acc[i][j][e] : full[i][j][e];
+          }
+        }
+      }
+      __syncthreads();  // the ring is free for the epilogue
+    }
+  }
 }
 
 }  // namespace pinsage
