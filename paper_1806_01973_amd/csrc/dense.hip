@@ -268,12 +268,6 @@ __device__ __forceinline__ void rows_block(const DenseLaunch& a, int block, int 
         const int cols = a.N - n;
         if (m >= valid || cols <= 0) return;
         const int64_t r = m0 + m;
-        if constexpr (!BF16) {
-          const float* const b = reinterpret_cast<const float*>(Bg);
-          redo_not_finite(v, cols < 4 ? cols : 4, reinterpret_cast<const float*>(Ap) + m * a.lda, 1,
-                          C::B_COL ? b + n : b + n * a.ldb, C::B_COL ? a.ldb : 1,
-                          C::B_COL ? 1 : a.ldb, a.K);
-        }
 #pragma unroll
         for (int e = 0; e < V; ++e) v[e] += bias[e];
         if (a.U)
@@ -541,9 +535,6 @@ __device__ __forceinline__ void dw_block(const DenseGradLaunch& a, int block, in
       [&](int m, int nn, float (&v)[V], Nothing) __attribute__((always_inline)) {
         const int cols = vk - nn;
         if (m >= vn || cols <= 0) return;
-        if constexpr (!BF16)
-          redo_not_finite(v, cols < 4 ? cols : 4, reinterpret_cast<const float*>(Z) + m, a.lddz,
-                          reinterpret_cast<const float*>(X) + nn, a.ldx, 1, rows);
         const int64_t at = (int64_t)(n0 + m) * a.K + k0 + nn;
         if (part) write_row<false>(part, at, cols, v);
         else write_row<BF16>(out, at, cols, v);

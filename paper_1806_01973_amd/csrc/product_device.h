@@ -13,10 +13,8 @@
 //   kF32    fp32 in memory, split on the way to the MFMAs into three bf16 parts (24
 //           significand bits), eight MFMAs, the leading products in sums of their
 //           own: what is left out is below 2^-33 of a product (split_device.h).
-//           Elements of rows and columns that the parts do not cover come from fp32
-//           MFMAs. Infinities and NaN, and values that round to a bf16 infinity,
-//           make an element that is not finite; the caller takes such elements from
-//           redo_not_finite.
+//           Elements of rows and columns that the parts do not cover, and sums that
+//           are not finite, come from fp32 MFMAs.
 // Sums run in fp32, chunks in order, so an element's bits follow from its row,
 // its column and the k range alone, whatever tile it lies in.
 #pragma once
@@ -285,27 +283,5 @@ __device__ __forceinline__ void product_rows_cols(const TileSums<C>& sums, unsig
 }
 
 struct Nothing {};
-
-// Of four elements of a row, `cols` of which exist, those that a split product left
-// without a finite value, again as fp32 dot products over `count` columns of k (a:
-// the row, b: the first of the four columns, b_next apart).
-__device__ __forceinline__ void redo_not_finite(float (&v)[4], int cols, const float* a,
-                                                int64_t a_step, const float* b, int64_t b_step,
-                                                int64_t b_next, int64_t count) {
-  const float probe = fmaf(v[0], 0.0f, fmaf(v[1], 0.0f, fmaf(v[2], 0.0f, v[3] * 0.0f)));
-  if (probe == 0.0f) return;
-#pragma unroll 1
-  for (int e = 0; e < cols; ++e) {
-    const float old = e == 0 ? v[0] : (e == 1 ? v[1] : (e == 2 ? v[2] : v[3]));
-    if (fabsf(old) < INFINITY) continue;
-    float s = 0.0f;
-#pragma unroll 1
-    for (int64_t k = 0; k < count; ++k) s = fmaf(a[k * a_step], b[e * b_next + k * b_step], s);
-    v[0] = e == 0 ? s : v[0];
-    v[1] = e == 1 ? s : v[1];
-    v[2] = e == 2 ? s : v[2];
-    v[3] = e == 3 ? s : v[3];
-  }
-}
 
 }  // namespace pinsage

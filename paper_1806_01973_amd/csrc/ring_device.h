@@ -18,8 +18,10 @@
 // fp32 values are split into their three bf16 parts after the LDS read, among the
 // MFMAs of the step before: 7 VALU instructions a value, twice per value and tile
 // with 64 x 64 wave tiles, under 8 MFMAs per product, and the least magnitudes are
-// kept. A tile of which the parts do not cover some pair of rows (split_covers) is
-// formed again with fp32 MFMAs.
+// kept. A tile of which the parts do not cover some pair of rows (split_covers), or of
+// which some sum is not finite, is formed again with fp32 MFMAs: twice a call's time
+// when it is all of them (4,096 x 512 -> 512 28 and 49 us, gradients 61 and 92;
+// gradients of 100,003 x 256 -> 512 448 and 821).
 //
 // What bounds large products are the MFMAs, in 63% of the cycles of 8,192 cubed by
 // 256 x 256 (counted when it took 943 us; it takes 878), and the clock, which power holds
@@ -491,7 +493,16 @@ __device__ __forceinline__ void tile_sums(const Operand& A, const Operand& B, in
     for (int i = 0; i < C::TM; ++i)
 #pragma unroll
       for (int j = 0; j < C::TN; ++j) acc[i][j] += small[i][j];
-    covered = split_covers(wave_min_key(key_a), wave_min_key(key_b));
+    // Infinities, NaN and values or sums that round to an infinity show in the results.
+    float probe = 0.0f;
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) probe = fmaf(acc[i][j][e], 0.0f, probe);
+    covered = split_covers(wave_min_key(key_a), wave_min_key(key_b)) &&
+              __ballot(probe != 0.0f) == 0ull;
     if (lane == 0) reinterpret_cast<uint32_t*>(smem + C::FLAGS)[wave] = !covered;
   }
   __syncthreads();
@@ -502,8 +513,8 @@ __device__ __forceinline__ void tile_sums(const Operand& A, const Operand& B, in
     if (again) {
       // The tile again with fp32 MFMAs (operand q of a step pairs half-wave h with its
       // column 8 h + q), a chunk in flight. Each element then follows from its own row
-      // and column alone: split where those are covered, else fp32, so that it does not
-      // depend on the tile it lies in.
+      // and column alone: split where those are covered and the sum is finite, else fp32,
+      // so that it does not depend on the tile it lies in.
       f32x16 full[C::TM][C::TN];
       uint32_t least_a[C::TM], least_b[C::TN];
 #pragma unroll
@@ -564,7 +575,11 @@ __device__ __forceinline__ void tile_sums(const Operand& A, const Operand& B, in
                 (uint32_t)__shfl((int)least_b[j], 8 * (e >> 2) + 4 * half + (e & 3));
 #pragma unroll
             for (int i = 0; i < C::TM; ++i)
-              acc[i][j][e] = split_covers(least_a[i], kb) ? acc[i][j][e] : full[i][j][e];
+            {
+              const float x = acc[i][j][e];
+              acc[i][j][e] =
+                  split_covers(least_a[i], kb) && fabsf(x) < INFINITY ? x : full[i][j][e];
+            }
           }
         }
       }
