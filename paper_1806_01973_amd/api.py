@@ -3,6 +3,11 @@
 Argument marshalling only: PyTorch provides device memory and the current HIP
 stream; every step of the hot path runs in the library's gfx950 kernels. The
 functions mirror the C entry points of include/pinsage.h.
+
+A call runs on `stream`, or on the current stream. The memory that it allocates,
+workspaces and outputs that are not given, belongs to that stream; inputs have to be
+ready on it, and outputs are used on another after a wait, as with any tensor made
+under torch.cuda.stream(stream).
 """
 
 from __future__ import annotations
@@ -24,6 +29,15 @@ def _ptr(t: Optional[torch.Tensor]):
 def _stream(stream: Optional[torch.cuda.Stream]):
     s = stream if stream is not None else torch.cuda.current_stream()
     return ctypes.c_void_p(s.cuda_stream)
+
+
+def _empty(shape, dtype: torch.dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """Memory for a call on `stream`: from that stream's own, so that what is dropped when the
+    call returns goes only to work that follows it there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _dev(t: torch.Tensor, name: str, dtype=None) -> torch.Tensor:
@@ -76,7 +90,7 @@ class DeviceGraph:
         self.walk_table = None
         L.check(L.lib().pinsage_walk_table_size(ctypes.byref(self.struct()), ctypes.byref(n)),
                 "pinsage_walk_table_size")
-        table = torch.empty(max(1, n.value), dtype=torch.uint8, device=self.col.device)
+        table = _empty(max(1, n.value), torch.uint8, self.col.device, stream)
         L.check(L.lib().pinsage_build_walk_table(ctypes.byref(self.struct()), table.data_ptr(),
                                                  table.numel(), _stream(stream)),
                 "pinsage_build_walk_table")
@@ -112,10 +126,11 @@ class Neighborhoods:
                                self.weights.data_ptr() if self.weights is not None else None)
 
     @staticmethod
-    def empty(rows: int, T: int, weights: bool = True, device="cuda") -> "Neighborhoods":
-        return Neighborhoods(torch.empty((rows, T), dtype=torch.int32, device=device),
-                             torch.empty((rows, T), dtype=torch.uint16, device=device),
-                             torch.empty((rows, T), dtype=torch.float32, device=device)
+    def empty(rows: int, T: int, weights: bool = True, device="cuda",
+              stream=None) -> "Neighborhoods":
+        return Neighborhoods(_empty((rows, T), torch.int32, device, stream),
+                             _empty((rows, T), torch.uint16, device, stream),
+                             _empty((rows, T), torch.float32, device, stream)
                              if weights else None)
 
 
@@ -178,14 +193,14 @@ def output_mlp(mlp: DeviceMLP, h: torch.Tensor, out: Optional[torch.Tensor] = No
     h = _dev(h, "h", mlp.dtype)
     n = int(h.shape[0])
     if out is None:
-        out = torch.empty((n, mlp.d_out), dtype=mlp.dtype, device=h.device)
+        out = _empty((n, mlp.d_out), mlp.dtype, h.device, stream)
     _dev(out, "out", mlp.dtype)
     m = mlp.struct()
     need = ctypes.c_size_t(0)
     L.check(L.lib().pinsage_output_mlp_workspace_size(ctypes.byref(m), n, ctypes.byref(need)),
             "pinsage_output_mlp_workspace_size")
     if workspace is None:
-        workspace = torch.empty(max(1, int(need.value)), dtype=torch.uint8, device=h.device)
+        workspace = _empty(max(1, int(need.value)), torch.uint8, h.device, stream)
     L.check(L.lib().pinsage_output_mlp(ctypes.byref(m), _ptr(h), n, _ptr(out), _ptr(workspace),
                                        workspace.numel(), _stream(stream)),
             "pinsage_output_mlp")
@@ -201,8 +216,8 @@ def build_neighborhoods(graph: DeviceGraph, walks: int, hops: int, T: int, seed:
     if sources is not None:
         sources = _dev(sources, "sources", torch.int32)
     rows = graph.num_nodes if sources is None else int(sources.numel())
-    nb = out if out is not None else Neighborhoods.empty(rows, T, weights, graph.col.device)
-    steps = torch.empty(1, dtype=torch.int64, device=graph.col.device) if count_steps else None
+    nb = out if out is not None else Neighborhoods.empty(rows, T, weights, graph.col.device, stream)
+    steps = _empty(1, torch.int64, graph.col.device, stream) if count_steps else None
     g, wp, ns = graph.struct(), L.WalkParams(seed, walks, hops, T), nb.struct()
     st = lib.pinsage_build_neighborhoods(ctypes.byref(g), ctypes.byref(wp), _ptr(sources), rows,
                                          ctypes.byref(ns), _ptr(steps), _stream(stream))
@@ -220,15 +235,14 @@ def hard_negatives(graph: DeviceGraph, queries: torch.Tensor, k: int, seed: int,
     queries = _dev(queries, "queries", torch.int32)
     n = int(queries.numel())
     if out is None:
-        out = torch.empty((n, k), dtype=torch.int32, device=queries.device)
-    steps = torch.empty(1, dtype=torch.int64, device=queries.device) if count_steps else None
+        out = _empty((n, k), torch.int32, queries.device, stream)
+    steps = _empty(1, torch.int64, queries.device, stream) if count_steps else None
     g = graph.struct()
     hp = L.HardNegativeParams(seed, walks, hops, rank_lo, rank_hi, k)
     need = ctypes.c_size_t(0)
     L.check(lib.pinsage_hard_negatives_workspace_size(ctypes.byref(hp), n, ctypes.byref(need)),
             "pinsage_hard_negatives_workspace_size")
-    ws = (torch.empty(int(need.value), dtype=torch.uint8, device=queries.device)
-          if need.value else None)
+    ws = _empty(int(need.value), torch.uint8, queries.device, stream) if need.value else None
     st = lib.pinsage_hard_negatives(ctypes.byref(g), ctypes.byref(hp), _ptr(queries), n, _ptr(out),
                                     _ptr(steps), _ptr(ws), int(need.value), _stream(stream))
     L.check(st, "pinsage_hard_negatives")
@@ -257,11 +271,11 @@ def convolve_layer(layer: DeviceLayer, h_in: torch.Tensor, n_transform: int, nbr
         n_transform = int(transform_rows.numel())
     n_out = nbr.rows
     if out is None:
-        out = torch.empty((n_out, layer.d_out), dtype=layer.dtype, device=h_in.device)
+        out = _empty((n_out, layer.d_out), layer.dtype, h_in.device, stream)
     _dev(out, "out", layer.dtype)
     need = convolve_workspace_size(layer, n_transform, n_out)
     if workspace is None:
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=h_in.device)
+        workspace = _empty(max(need, 1), torch.uint8, h_in.device, stream)
     ns = nbr.struct()
     st = lib.pinsage_convolve_layer(ctypes.byref(layer.struct()), _ptr(h_in), h_in.shape[0],
                                     n_transform, _ptr(transform_rows), ctypes.byref(ns),
@@ -363,7 +377,7 @@ def build_graph_neighborhoods(graph: DeviceGraph, T: int, seed: int,
     if sources is not None:
         sources = _dev(sources, "sources", torch.int32)
     rows = graph.num_nodes if sources is None else int(sources.numel())
-    nb = out if out is not None else Neighborhoods.empty(rows, T, weights, graph.col.device)
+    nb = out if out is not None else Neighborhoods.empty(rows, T, weights, graph.col.device, stream)
     g, ns = graph.struct(), nb.struct()
     st = L.lib().pinsage_build_graph_neighborhoods(ctypes.byref(g), seed, _ptr(sources), rows,
                                                    ctypes.byref(ns), _stream(stream))
@@ -408,8 +422,9 @@ class EmbedAllBipartite:
 
 def embed_all(graph: DeviceGraph, layers: List[DeviceLayer], x: torch.Tensor, walks: int,
               hops: int, T: int, seed: int, stream=None):
-    job = EmbedAll(graph, layers, walks, hops, T, seed)
-    out = job.run(x, stream)
+    with torch.cuda.stream(stream):  # the job's buffers are the call's: see _empty
+        job = EmbedAll(graph, layers, walks, hops, T, seed)
+        out = job.run(x)
     return job.nbr, out, job.steps
 
 
@@ -427,8 +442,8 @@ def max_margin_loss(zq: torch.Tensor, zpos: torch.Tensor, zneg: torch.Tensor, ma
         if zhard.dim() != 3 or zhard.shape[0] != B or zhard.shape[2] != d:
             raise ValueError("zhard must be [B][k][d]")
         k = int(zhard.shape[1])
-    loss = torch.empty(1, dtype=torch.float32, device=zq.device)
-    per = torch.empty(B, dtype=torch.float32, device=zq.device)
+    loss = _empty(1, torch.float32, zq.device, stream)
+    per = _empty(B, torch.float32, zq.device, stream)
     st = L.lib().pinsage_max_margin_loss(_ptr(zq), _ptr(zpos), B, _ptr(zneg), zneg.shape[0],
                                          _ptr(zhard), k, d, _dtype_code(dt), margin, _ptr(loss),
                                          _ptr(per), _stream(stream))
@@ -582,11 +597,11 @@ def dense_forward(x: torch.Tensor, W: torch.Tensor, b: Optional[torch.Tensor] = 
     ldx = _rows(x, "x", n, d.d_in, x.dtype)
     ldr = _rows(residual, "residual", n, d.d_out, x.dtype) if residual is not None else 0
     if out is None:
-        out = torch.empty((n, d.d_out), dtype=x.dtype, device=x.device)
+        out = _empty((n, d.d_out), x.dtype, x.device, stream)
         ldy = d.d_out
     else:
         ldy = _rows(out, "out", n, d.d_out, x.dtype)
-    u = torch.empty((n, d.d_out), dtype=x.dtype, device=x.device) if want_preact else None
+    u = _empty((n, d.d_out), x.dtype, x.device, stream) if want_preact else None
     st = L.lib().pinsage_dense_forward(ctypes.byref(d), x.data_ptr(), n, ldx,
                                        residual.data_ptr() if residual is not None else None, ldr,
                                        u.data_ptr() if want_preact else None, d.d_out,
@@ -614,15 +629,15 @@ def dense_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor,
         if u is None:
             raise ValueError("u is needed for the gradient through an activation")
         ldu = _rows(u, "u", n, d.d_out, x.dtype)
-    dx = torch.empty((n, d.d_in), dtype=x.dtype, device=x.device) if need_dx else None
-    dW = torch.empty(W.shape, dtype=x.dtype, device=x.device) if need_dW else None
-    db = torch.empty(W.shape[:-1], dtype=torch.float32, device=x.device) if need_db else None
+    dx = _empty((n, d.d_in), x.dtype, x.device, stream) if need_dx else None
+    dW = _empty(W.shape, x.dtype, x.device, stream) if need_dW else None
+    db = _empty(W.shape[:-1], torch.float32, x.device, stream) if need_db else None
     if workspace is None:
         need = ctypes.c_size_t(0)
         L.check(L.lib().pinsage_dense_backward_workspace_size(ctypes.byref(d), n,
                                                               ctypes.byref(need)),
                 "pinsage_dense_backward_workspace_size")
-        workspace = torch.empty(max(1, need.value), dtype=torch.uint8, device=x.device)
+        workspace = _empty(max(1, need.value), torch.uint8, x.device, stream)
     st = L.lib().pinsage_dense_backward(ctypes.byref(d), dy.data_ptr(), lddy, x.data_ptr(), ldx,
                                         u.data_ptr() if u is not None else None, ldu, n,
                                         _ptr(dx), d.d_in, _ptr(dW), _ptr(db),
@@ -653,11 +668,11 @@ def _newton_schulz(t: torch.Tensor, name: str, steps: int, coefficients, eps: fl
                           c, eps)
 
 
-def _newton_schulz_workspace(p: L.NewtonSchulz, device) -> torch.Tensor:
+def _newton_schulz_workspace(p: L.NewtonSchulz, device, stream) -> torch.Tensor:
     need = ctypes.c_size_t(0)
     L.check(L.lib().pinsage_newton_schulz_workspace_size(ctypes.byref(p), ctypes.byref(need)),
             "pinsage_newton_schulz_workspace_size")
-    return torch.empty(max(1, need.value), dtype=torch.uint8, device=device)
+    return _empty(max(1, need.value), torch.uint8, device, stream)
 
 
 def orthogonalize(g: torch.Tensor, steps: int = 5, coefficients=NEWTON_SCHULZ, eps: float = 1e-7,
@@ -668,11 +683,11 @@ def orthogonalize(g: torch.Tensor, steps: int = 5, coefficients=NEWTON_SCHULZ, e
     orientation with fewer rows than columns)."""
     p = _newton_schulz(g, "g", steps, coefficients, eps)
     if out is None:
-        out = torch.empty_like(g)
+        out = _empty(g.shape, g.dtype, g.device, stream)
     elif _dev(out, "out", g.dtype).shape != g.shape:
         raise ValueError("out must have g's shape")
     if workspace is None:
-        workspace = _newton_schulz_workspace(p, g.device)
+        workspace = _newton_schulz_workspace(p, g.device, stream)
     st = L.lib().pinsage_orthogonalize(ctypes.byref(p), g.data_ptr(), out.data_ptr(),
                                        workspace.data_ptr(), workspace.numel(),
                                        _raw_stream(stream, g.device))
@@ -704,7 +719,7 @@ def muon_step(W: torch.Tensor, grad: torch.Tensor, momentum: torch.Tensor, lr: f
         scale = max(1.0, p.rows / p.cols) ** 0.5
     m = L.Muon(lr, beta, weight_decay, scale, 1 if nesterov else 0)
     if workspace is None:
-        workspace = _newton_schulz_workspace(p, W.device)
+        workspace = _newton_schulz_workspace(p, W.device, stream)
     st = L.lib().pinsage_muon_step(ctypes.byref(p), ctypes.byref(m), W.data_ptr(),
                                    grad.data_ptr(), momentum.data_ptr(), W_out.data_ptr(),
                                    momentum_out.data_ptr(), workspace.data_ptr(),
