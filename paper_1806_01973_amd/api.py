@@ -50,6 +50,13 @@ def _dev(t: torch.Tensor, name: str, dtype=None) -> torch.Tensor:
     return t
 
 
+def _workspace(t: Optional[torch.Tensor], need: int, device, stream) -> torch.Tensor:
+    """The caller's workspace, or `need` bytes for this call."""
+    if t is None:
+        return _empty(max(1, need), torch.uint8, device, stream)
+    return _dev(t, "workspace")
+
+
 def _dtype_code(dt: torch.dtype) -> int:
     if dt == torch.float32:
         return L.PINSAGE_F32
@@ -199,8 +206,7 @@ def output_mlp(mlp: DeviceMLP, h: torch.Tensor, out: Optional[torch.Tensor] = No
     need = ctypes.c_size_t(0)
     L.check(L.lib().pinsage_output_mlp_workspace_size(ctypes.byref(m), n, ctypes.byref(need)),
             "pinsage_output_mlp_workspace_size")
-    if workspace is None:
-        workspace = _empty(max(1, int(need.value)), torch.uint8, h.device, stream)
+    workspace = _workspace(workspace, int(need.value), h.device, stream)
     L.check(L.lib().pinsage_output_mlp(ctypes.byref(m), _ptr(h), n, _ptr(out), _ptr(workspace),
                                        workspace.numel(), _stream(stream)),
             "pinsage_output_mlp")
@@ -274,8 +280,7 @@ def convolve_layer(layer: DeviceLayer, h_in: torch.Tensor, n_transform: int, nbr
         out = _empty((n_out, layer.d_out), layer.dtype, h_in.device, stream)
     _dev(out, "out", layer.dtype)
     need = convolve_workspace_size(layer, n_transform, n_out)
-    if workspace is None:
-        workspace = _empty(max(need, 1), torch.uint8, h_in.device, stream)
+    workspace = _workspace(workspace, need, h_in.device, stream)
     ns = nbr.struct()
     st = lib.pinsage_convolve_layer(ctypes.byref(layer.struct()), _ptr(h_in), h_in.shape[0],
                                     n_transform, _ptr(transform_rows), ctypes.byref(ns),
@@ -638,6 +643,8 @@ def dense_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor,
                                                               ctypes.byref(need)),
                 "pinsage_dense_backward_workspace_size")
         workspace = _empty(max(1, need.value), torch.uint8, x.device, stream)
+    else:
+        _dev(workspace, "workspace")
     st = L.lib().pinsage_dense_backward(ctypes.byref(d), dy.data_ptr(), lddy, x.data_ptr(), ldx,
                                         u.data_ptr() if u is not None else None, ldu, n,
                                         _ptr(dx), d.d_in, _ptr(dW), _ptr(db),
@@ -668,7 +675,9 @@ def _newton_schulz(t: torch.Tensor, name: str, steps: int, coefficients, eps: fl
                           c, eps)
 
 
-def _newton_schulz_workspace(p: L.NewtonSchulz, device, stream) -> torch.Tensor:
+def _newton_schulz_workspace(p: L.NewtonSchulz, workspace, device, stream) -> torch.Tensor:
+    if workspace is not None:
+        return _dev(workspace, "workspace")
     need = ctypes.c_size_t(0)
     L.check(L.lib().pinsage_newton_schulz_workspace_size(ctypes.byref(p), ctypes.byref(need)),
             "pinsage_newton_schulz_workspace_size")
@@ -686,8 +695,7 @@ def orthogonalize(g: torch.Tensor, steps: int = 5, coefficients=NEWTON_SCHULZ, e
         out = _empty(g.shape, g.dtype, g.device, stream)
     elif _dev(out, "out", g.dtype).shape != g.shape:
         raise ValueError("out must have g's shape")
-    if workspace is None:
-        workspace = _newton_schulz_workspace(p, g.device, stream)
+    workspace = _newton_schulz_workspace(p, workspace, g.device, stream)
     st = L.lib().pinsage_orthogonalize(ctypes.byref(p), g.data_ptr(), out.data_ptr(),
                                        workspace.data_ptr(), workspace.numel(),
                                        _raw_stream(stream, g.device))
@@ -718,8 +726,7 @@ def muon_step(W: torch.Tensor, grad: torch.Tensor, momentum: torch.Tensor, lr: f
     if scale is None:
         scale = max(1.0, p.rows / p.cols) ** 0.5
     m = L.Muon(lr, beta, weight_decay, scale, 1 if nesterov else 0)
-    if workspace is None:
-        workspace = _newton_schulz_workspace(p, W.device, stream)
+    workspace = _newton_schulz_workspace(p, workspace, W.device, stream)
     st = L.lib().pinsage_muon_step(ctypes.byref(p), ctypes.byref(m), W.data_ptr(),
                                    grad.data_ptr(), momentum.data_ptr(), W_out.data_ptr(),
                                    momentum_out.data_ptr(), workspace.data_ptr(),
