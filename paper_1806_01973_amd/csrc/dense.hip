@@ -54,8 +54,10 @@ __device__ __forceinline__ void grad_through(float (&dy)[N], const float (&u)[N]
   } else if (act == kActGelu) {
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      const float q = kGeluCube * u[e] * u[e], s = sigmoid(kGelu2 * u[e] * (1.0f + q));
-      dy[e] *= s + u[e] * s * (1.0f - s) * kGelu2 * (1.0f + 3.0f * q);
+      // 0 and 1 long before 64, where u^2 could overflow beside a factor that is 0. NaN stays.
+      const float x = fabsf(u[e]) > 64.0f ? copysignf(64.0f, u[e]) : u[e];
+      const float q = kGeluCube * x * x, s = sigmoid(kGelu2 * x * (1.0f + q));
+      dy[e] *= s + x * s * (1.0f - s) * kGelu2 * (1.0f + 3.0f * q);
     }
   } else if (act == kActSilu) {
 #pragma unroll

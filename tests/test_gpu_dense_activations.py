@@ -1,0 +1,33 @@
+"""GPU: activations and their slopes far out, element by element.
+
+One input and a weight of 1 leave u = x exactly, and dy = 1 shows the slope.
+"""
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+def ps():
+    import paper_1806_01973_amd
+    return paper_1806_01973_amd
+
+
+FAR = [64.0, 1e4, 1e13, 5e18, 1e19, 9e19, 1e25, 3e38]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
+def test_values_and_slopes_far_out(act, dtype):
+    """From 64 on every activation is the identity to the right and zero to the left,
+    its slope 1 and 0, to half of fp32's last place at 1."""
+    half = 2.0 ** -24
+    u = torch.tensor(FAR + [-v for v in FAR], dtype=dtype, device="cuda")[:, None]
+    one = torch.ones(1, 1, dtype=dtype, device="cuda")
+    dx, _, db = ps().dense_backward(torch.ones_like(u), u, one, u, act, need_dW=False)
+    right = (u > 0).float()
+    assert ((dx.float() - right).abs() <= half).all()
+    assert abs(db.item() - len(FAR)) <= 2 * len(FAR) * half
+    y = ps().dense_forward(u, one, activation=act).float()
+    assert ((y - u.float() * right).abs() <= half).all()
