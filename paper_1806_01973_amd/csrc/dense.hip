@@ -24,13 +24,17 @@ namespace {
 constexpr float kGelu2 = 1.5957691216057308f;  // 2 sqrt(2 / pi)
 constexpr float kGeluCube = 0.044715f;
 
-// The reciprocal instruction is within 1 unit in the last place.
+// For bf16 results the exponential whose relative error grows with |x| (2^-20 at 10)
+// and the reciprocal instruction (1 unit in the last place) are near enough; fp32 takes
+// the exact forms.
+template <bool BF16>
 __device__ __forceinline__ float sigmoid(float x) {
-  return __builtin_amdgcn_rcpf(1.0f + __expf(-x));
+  if constexpr (BF16) return __builtin_amdgcn_rcpf(1.0f + __expf(-x));
+  else return 1.0f / (1.0f + expf(-x));
 }
 
 // One branch for all values, not one for each.
-template <int N>
+template <bool BF16, int N>
 __device__ __forceinline__ void activate(float (&u)[N], int act) {
   if (act == kActRelu) {
 #pragma unroll
@@ -38,15 +42,15 @@ __device__ __forceinline__ void activate(float (&u)[N], int act) {
   } else if (act == kActGelu) {
 #pragma unroll
     for (int e = 0; e < N; ++e)
-      u[e] *= sigmoid(kGelu2 * (u[e] + kGeluCube * u[e] * u[e] * u[e]));
+      u[e] *= sigmoid<BF16>(kGelu2 * (u[e] + kGeluCube * u[e] * u[e] * u[e]));
   } else if (act == kActSilu) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) u[e] *= sigmoid(u[e]);
+    for (int e = 0; e < N; ++e) u[e] *= sigmoid<BF16>(u[e]);
   }
 }
 
 // dy becomes dy * act'(u).
-template <int N>
+template <bool BF16, int N>
 __device__ __forceinline__ void grad_through(float (&dy)[N], const float (&u)[N], int act) {
   if (act == kActRelu) {
 #pragma unroll
@@ -56,13 +60,13 @@ __device__ __forceinline__ void grad_through(float (&dy)[N], const float (&u)[N]
     for (int e = 0; e < N; ++e) {
       // 0 and 1 long before 64, where u^2 could overflow beside a factor that is 0. NaN stays.
       const float x = fabsf(u[e]) > 64.0f ? copysignf(64.0f, u[e]) : u[e];
-      const float q = kGeluCube * x * x, s = sigmoid(kGelu2 * x * (1.0f + q));
+      const float q = kGeluCube * x * x, s = sigmoid<BF16>(kGelu2 * x * (1.0f + q));
       dy[e] *= s + x * s * (1.0f - s) * kGelu2 * (1.0f + 3.0f * q);
     }
   } else if (act == kActSilu) {
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      const float s = sigmoid(u[e]);
+      const float s = sigmoid<BF16>(u[e]);
       dy[e] *= s * (1.0f + u[e] * (1.0f - s));
     }
   }
@@ -274,7 +278,7 @@ __device__ __forceinline__ void rows_block(const DenseLaunch& a, int block, int 
         for (int e = 0; e < V; ++e) v[e] += bias[e];
         if (a.U)
           write_row<BF16>(static_cast<unsigned char*>(a.U) + r * a.ldu * C::ESZ, n, cols, v);
-        activate(v, a.act);
+        activate<BF16>(v, a.act);
 #pragma unroll
         for (int e = 0; e < V; ++e) v[e] += x.v[e];
         write_row<BF16>(static_cast<unsigned char*>(a.C) + r * a.ldc * C::ESZ, n, cols, v);
@@ -390,7 +394,7 @@ __device__ __forceinline__ void few_rows(const DenseLaunch& a, const unsigned ch
         for (int e = 0; e < 4; ++e) v[e] += w[e];
       }
       if (a.U) write_row<BF16>(static_cast<unsigned char*>(a.U) + r * a.ldu * ESZ, n, cols, v);
-      activate(v, a.act);
+      activate<BF16>(v, a.act);
       if (a.residual && !orphans) {
         float w[4];
         read_row<BF16>(static_cast<const unsigned char*>(a.residual) + r * a.ldr * ESZ, n, cols, w);
@@ -469,7 +473,7 @@ __global__ __launch_bounds__(256) void dense_dz_kernel(DenseGradLaunch a, int la
       for (int k = 0; k < DEEP; ++k) {
         const int64_t q = r + k * step;
         if (q >= rows) break;
-        if (u) grad_through(d[k], x[k], a.act);
+        if (u) grad_through<BF16>(d[k], x[k], a.act);
         if (a.dz) write_row<BF16>(dz + q * a.lddz * ESZ, n, have, d[k]);
 #pragma unroll
         for (int e = 0; e < V; ++e) s[e] += d[k][e];

@@ -31,3 +31,13 @@ def test_values_and_slopes_far_out(act, dtype):
     assert abs(db.item() - len(FAR)) <= 2 * len(FAR) * half
     y = ps().dense_forward(u, one, activation=act).float()
     assert ((y - u.float() * right).abs() <= half).all()
+
+
+@pytest.mark.parametrize("n", [40, 3000])
+def test_silu_keeps_its_relative_accuracy(n):
+    """u / (1 + exp(-u)): the exponential is within 2^-22 of itself, the sum, the
+    quotient and the product within 2^-24 each, at any u whose exponential is finite."""
+    u = torch.linspace(-86.0, 86.0, n)[:, None]
+    y = ps().dense_forward(u.cuda(), torch.ones(1, 1).cuda(), activation="silu").double().cpu()
+    want = u.double() / (1 + torch.exp(-u.double()))
+    assert ((y - want).abs() <= 2.0 ** -21 * want.abs()).all()
