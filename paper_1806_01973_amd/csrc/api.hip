@@ -6,6 +6,7 @@
 // back).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -1756,6 +1757,43 @@ DenseWs dense_ws(const pinsage_dense_t* d, int64_t n) {
   return w;
 }
 
+// The largest |p(x)| over [0, top] of p(x) = a x + b x^3 + c x^5: at the end, or where
+// p'(x) = a + 3 b x^2 + 5 c x^4 is zero.
+double newton_reach(double a, double b, double c, double top) {
+  auto value = [&](double x) { return std::fabs(x * (a + x * x * (b + x * x * c))); };
+  double most = value(top);
+  auto turn = [&](double square) {
+    if (square > 0 && square < top * top) most = std::max(most, value(std::sqrt(square)));
+  };
+  if (c == 0) {
+    if (b != 0) turn(-a / (3 * b));
+  } else {
+    const double d = 9 * b * b - 20 * a * c;
+    if (d >= 0) {
+      turn((-3 * b + std::sqrt(d)) / (10 * c));
+      turn((-3 * b - std::sqrt(d)) / (10 * c));
+    }
+  }
+  return most;
+}
+
+// Whether what the iteration keeps (X, A = X X^T, b A + c A A and A X) stays below 15.5,
+// where its fp16 parts end at 16, for every matrix: no entry exceeds the largest singular
+// value, X's are at most 1 at first, and each step moves them by a x + b x^3 + c x^5.
+bool newton_in_range(const pinsage_newton_schulz_t* p) {
+  const double a = p->a, b = p->b, c = p->c, most = 15.5;
+  double top = 1.0;
+  for (int k = 0; k < p->steps; ++k) {
+    const double square = top * top;
+    double middle = std::fabs(square * (b + c * square));
+    const double turn = c != 0 ? -b / (2 * c) : 0.0;
+    if (turn > 0 && turn < square) middle = std::max(middle, std::fabs(turn * (b + c * turn)));
+    if (!(square <= most && middle <= most && square * top <= most)) return false;
+    top = newton_reach(a, b, c, top);
+  }
+  return top <= most;
+}
+
 int check_newton(const pinsage_newton_schulz_t* p) {
   if (!p) return fail(PINSAGE_EINVAL, "params are NULL");
   if (p->dtype != PINSAGE_F32 && p->dtype != PINSAGE_BF16)
@@ -1770,6 +1808,9 @@ int check_newton(const pinsage_newton_schulz_t* p) {
   if (!(p->eps >= 0.0f) || !std::isfinite(p->eps) || !std::isfinite(p->a) ||
       !std::isfinite(p->b) || !std::isfinite(p->c))
     return fail(PINSAGE_EINVAL, "coefficients and eps must be finite, eps >= 0");
+  if (!newton_in_range(p))
+    return fail(PINSAGE_EUNSUPPORTED, "coefficients (%g, %g, %g) can take %d steps past 16", p->a,
+                p->b, p->c, p->steps);
   return PINSAGE_OK;
 }
 
