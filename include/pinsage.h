@@ -540,8 +540,8 @@ int pinsage_dense_backward_workspace_size(const pinsage_dense_t* layer, int64_t 
  * residual y serves as well); dx: device [n][d_in], rows lddx apart, or NULL;
  * dW: device [d_out][d_in] ([G] of them), dense, or NULL; db: device fp32
  * [d_out] ([G] of them) or NULL; a NULL output is not computed. dx, dW in the
- * storage dtype, rounded once from fp32 sums; dz is rounded to the storage
- * dtype for dx and dW (not for db). RELU's derivative at 0 is 0. Outputs
+ * storage dtype, rounded once from fp32 sums; for dx and dW dz is held in fp32,
+ * for bf16 storage to 2^-17 of itself. RELU's derivative at 0 is 0. Outputs
  * overlap no input. Sums are added in a fixed order. workspace: device, >=
  * pinsage_dense_backward_workspace_size bytes, 256-aligned. */
 int pinsage_dense_backward(const pinsage_dense_t* layer, const void* dy, int64_t lddy,

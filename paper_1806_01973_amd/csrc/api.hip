@@ -1739,10 +1739,11 @@ int check_dense(const pinsage_dense_t* d, int64_t n) {
   return PINSAGE_OK;
 }
 
-// Workspace of a backward pass: dz (where an activation makes it differ from
-// dy) | partial sums of db | partial sums of dW.
+// Workspace of a backward pass: dz (where an activation makes it differ from dy; in two
+// parts where bf16 does not hold it) | partial sums of db | partial sums of dW.
 struct DenseWs {
   int64_t lddz = 0, piece = 0;
+  int64_t dz_plane = 0;  // bytes; 0: dz in one part
   size_t dz = 0, db = 0, dw = 0;
   size_t total() const { return dz + db + dw; }
 };
@@ -1752,6 +1753,11 @@ DenseWs dense_ws(const pinsage_dense_t* d, int64_t n) {
   w.lddz = (d->d_out + 7) / 8 * 8;
   w.piece = dense_dw_piece(n, d->d_out, d->d_in, d->num_groups, d->dtype == PINSAGE_BF16);
   if (d->activation != PINSAGE_ACT_NONE) w.dz = align_up((size_t)n * w.lddz * elem_size(d->dtype));
+  // ReLU's dz is dy or 0, which bf16 holds.
+  if (d->dtype == PINSAGE_BF16 && d->activation > PINSAGE_ACT_RELU) {
+    w.dz_plane = (int64_t)w.dz;
+    w.dz *= 2;
+  }
   w.db = align_up((size_t)dense_bias_pieces(n, d->num_groups, dense_bias_rows(n, d->d_out, d->dtype == PINSAGE_BF16)) * d->d_out * 4);
   w.dw = align_up((size_t)dense_dw_parts(n, w.piece, d->num_groups) * d->d_out * d->d_in * 4);
   return w;
@@ -1923,6 +1929,7 @@ int pinsage_dense_backward(const pinsage_dense_t* layer, const void* dy, int64_t
   g.ldx = ldx;
   g.dz = through && (dx || dW) ? ws : nullptr;
   g.lddz = w.lddz;
+  g.dz_plane = g.dz ? w.dz_plane : 0;
   g.db = db;
   g.db_parts = db ? reinterpret_cast<float*>(ws + w.dz) : nullptr;
   g.bias_rows = dense_bias_rows(n, layer->d_out, layer->dtype == PINSAGE_BF16);
@@ -1948,6 +1955,7 @@ int pinsage_dense_backward(const pinsage_dense_t* layer, const void* dy, int64_t
   DenseLaunch a{};
   a.A = g.dz;
   a.lda = g.lddz;
+  a.a_plane = g.dz_plane;
   a.B = layer->W;
   a.ldb = layer->ldw;
   a.group_stride = layer->d_out * layer->ldw;

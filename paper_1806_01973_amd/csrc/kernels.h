@@ -269,9 +269,11 @@ enum DenseAct { kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3 };
 // group g holds rows offsets[g] .. offsets[g + 1] - 1 (device; null = one group) and
 // has B + g * group_stride, bias + g * N. Rows past the last group become zero.
 // Leading dimensions in elements; storage dtype bf16 or fp32, bias fp32.
+// A may come in two bf16 parts (bf16 storage), planes apart by a_plane bytes.
 struct DenseLaunch {
   const void* A;
   int64_t lda;
+  int64_t a_plane;       // 0: one part
   const void* B;
   int64_t ldb;
   int64_t group_stride;
@@ -305,6 +307,7 @@ struct DenseGradLaunch {
   int64_t ldx;
   void* dz;
   int64_t lddz;
+  int64_t dz_plane;  // bytes from dz's hi parts to its lo parts; 0: one part
   float* db;        // nullable
   float* db_parts;  // [dense_bias_pieces][N]; null when db is
   int bias_rows;    // rows per partial sum of db: dense_bias_rows

@@ -170,7 +170,7 @@ template <class C, int KIND, bool BF16>
 __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch a, NewtonWork w,
                                                                     int from, int tiles) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[C::LDS_BYTES];
-  static_assert(C::MEM_PLANES == kParts, "");
+  static_assert(C::A_PLANES == kParts && C::B_PLANES == kParts, "");
   constexpr bool kSymmetric = KIND == kGram || KIND == kSquare;
   const int64_t px = (int64_t)w.mp * w.np, pa = (int64_t)w.mp * w.mp;
   // Neighbouring tiles, and whole matrices of a batch, on one XCD.

@@ -7,6 +7,8 @@
 //
 // Modes:
 //   kBf16   bf16 in memory, one MFMA per product
+//   kBf16A2 the same, A in two bf16 parts (planes apart by `plane` bytes: 16
+//           significand bits), two MFMAs (lo, hi)
 //   kF16x2  two fp16 parts in memory (x = hi + lo, planes apart by `plane`
 //           bytes): 22 significand bits, three MFMAs (hi lo, lo hi, hi hi); for
 //           operands the caller keeps inside fp16's range
@@ -27,7 +29,7 @@ namespace pinsage {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-enum ProductMode { kBf16 = 0, kF16x2 = 2, kF32 = 3 };
+enum ProductMode { kBf16 = 0, kBf16A2 = 1, kF16x2 = 2, kF32 = 3 };
 
 // A tile's operand: `p` at the tile's first row (row operand, k = 0) or first
 // column (column operand, k = 0); `valid` rows exist from there (at least 1).
@@ -35,7 +37,7 @@ struct Operand {
   const void* p;
   int64_t ld;     // elements
   int valid;
-  int64_t plane;  // kF16x2: bytes from the hi plane to the lo plane
+  int64_t plane;  // two parts: bytes from the hi plane to the lo plane
   int before = 0;  // columns that exist before p
 };
 

@@ -53,15 +53,18 @@ struct RingCfg {
   static constexpr bool A_COL = A_COL_, B_COL = B_COL_;
   static constexpr int NWAVES = WAVES_M * WAVES_N, THREADS = 64 * NWAVES;
   static constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, TM = WM / 32, TN = WN / 32;
-  static constexpr int ESZ = MODE == kF32 ? 4 : 2, MEM_PLANES = MODE == kF16x2 ? 2 : 1;
-  static constexpr int PARTS = MODE == kF32 ? 3 : MEM_PLANES;  // of a fragment
+  static constexpr int ESZ = MODE == kF32 ? 4 : 2;
+  static constexpr int A_PLANES = MODE == kF16x2 || MODE == kBf16A2 ? 2 : 1;  // in memory
+  static constexpr int B_PLANES = MODE == kF16x2 ? 2 : 1;
+  static constexpr int A_PARTS = MODE == kF32 ? 3 : A_PLANES;  // of a fragment
+  static constexpr int B_PARTS = MODE == kF32 ? 3 : B_PLANES;
   static constexpr int A_PLANE = BM * BK * ESZ, B_PLANE = BN * BK * ESZ;
-  static constexpr int A_BYTES = A_PLANE * MEM_PLANES, B_BYTES = B_PLANE * MEM_PLANES;
+  static constexpr int A_BYTES = A_PLANE * A_PLANES, B_BYTES = B_PLANE * B_PLANES;
   static constexpr int STEPS = BK / 16;  // k steps of a chunk
   // One DMA instruction of a wave fills a group of 1 KB.
   static constexpr int A_GROUPS = A_PLANE / 1024, B_GROUPS = B_PLANE / 1024;  // per plane
-  static constexpr int DA = A_GROUPS * MEM_PLANES / NWAVES;  // of a wave, per chunk
-  static constexpr int DB = B_GROUPS * MEM_PLANES / NWAVES;
+  static constexpr int DA = A_GROUPS * A_PLANES / NWAVES;  // of a wave, per chunk
+  static constexpr int DB = B_GROUPS * B_PLANES / NWAVES;
   static constexpr int PENDING = (STAGES - 2) * (DA + DB) + AHEAD * DA;
   static constexpr int STAGE_LD = WN + 4;
   static constexpr int STAGE_BYTES = 32 * STAGE_LD * 4;
@@ -69,12 +72,11 @@ struct RingCfg {
   // kF32: behind the ring a word a wave, whether it wants the tile again.
   static constexpr int FLAGS = RING > NWAVES * STAGE_BYTES ? RING : NWAVES * STAGE_BYTES;
   static constexpr int LDS_BYTES = FLAGS + (MODE == kF32 ? 4 * NWAVES : 0);
-  static_assert(A_GROUPS * MEM_PLANES % NWAVES == 0 && B_GROUPS * MEM_PLANES % NWAVES == 0 &&
+  static_assert(A_GROUPS * A_PLANES % NWAVES == 0 && B_GROUPS * B_PLANES % NWAVES == 0 &&
                     A_GROUPS % DA == 0 && B_GROUPS % DB == 0,
                 "every wave serves one plane of each operand");
   static_assert(STAGES >= 2 && PENDING <= 63 && LDS_BYTES <= 160 * 1024, "");
-  static_assert(!REGS || (MEM_PLANES == 1 && AHEAD == 0), "");
-  static_assert(MODE != kF32 || AHEAD == 0, "");
+  static_assert((!REGS && MODE != kF32) || AHEAD == 0, "");
   static_assert(BK * ESZ == 64 || BK * ESZ == 128, "rows of 4 or 8 slots");
 };
 
@@ -134,7 +136,7 @@ __device__ __forceinline__ void tile_sums(const Operand& A, const Operand& B, in
                                           int64_t k1, unsigned char* smem, TileSums<C>& sums) {
   constexpr int BK = C::BK, ESZ = C::ESZ, VE = 16 / ESZ, STAGES = C::STAGES;
   constexpr int STAGES_A = STAGES + C::AHEAD;
-  constexpr int PARTS = C::PARTS, PLANES = C::MEM_PLANES, SLOTS = BK / VE;
+  constexpr int SLOTS = BK / VE;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int wm = wave / C::WAVES_N, wn = wave % C::WAVES_N;
@@ -291,10 +293,10 @@ __device__ __forceinline__ void tile_sums(const Operand& A, const Operand& B, in
   // ---- fragments ------------------------------------------------------------------
   const int frag_row = lane & 31, half = lane >> 5;
   struct Frags {
-    u32x4 a[C::TM][PARTS], b[C::TN][PARTS];
+    u32x4 a[C::TM][C::A_PARTS], b[C::TN][C::B_PARTS];
   };
   // Eight k of one row: a vector of 16-bit values, or two of fp32 (in parts 0 and 1).
-  auto read_row = [&](const unsigned char* tile, int r, int ks, u32x4 (&out)[PARTS])
+  auto read_row = [&](const unsigned char* tile, int r, int ks, auto& out)
       __attribute__((always_inline)) {
     const unsigned char* const row = tile + r * (BK * ESZ);
     const int s0 = (2 * ks + half) * (8 / VE), sw = ring_row_swizzle<SLOTS>(r);
@@ -303,7 +305,7 @@ __device__ __forceinline__ void tile_sums(const Operand& A, const Operand& B, in
   };
   // The same of a column operand: with 16-bit values a lane (j, c) of 16 reads k row
   // j's values 4 c .. 4 c + 3, twice for k and k + 4.
-  auto read_col = [&](const unsigned char* tile, int m0, int ks, int width, u32x4 (&out)[PARTS])
+  auto read_col = [&](const unsigned char* tile, int m0, int ks, int width, auto& out)
       __attribute__((always_inline)) {
     if constexpr (ESZ == 4) {
       const unsigned char* const at =
@@ -334,21 +336,24 @@ __device__ __forceinline__ void tile_sums(const Operand& A, const Operand& B, in
     const unsigned char* const tile = kOfA ? smem + (c % STAGES_A) * C::A_BYTES
                                            : smem + STAGES_A * C::A_BYTES + (c % STAGES) * C::B_BYTES;
     const int m = kOfA ? wm * C::WM + 32 * q : wn * C::WN + 32 * (q - C::TM);
-    u32x4(&to)[PARTS] = kOfA ? f.a[kOfA ? q : 0] : f.b[kOfA ? 0 : q - C::TM];
-    unroll<0, PLANES>([&](auto plane) __attribute__((always_inline)) {
-      constexpr int p = decltype(plane)::value;
-      const unsigned char* const from = tile + p * (kOfA ? C::A_PLANE : C::B_PLANE);
-      u32x4(&out)[PARTS] = to;
-      if constexpr (PLANES == 1) {
-        if constexpr (COL) read_col(from, m, ks, width, out);
-        else read_row(from, m + frag_row, ks, out);
-      } else {
-        u32x4 x[PARTS];
-        if constexpr (COL) read_col(from, m, ks, width, x);
-        else read_row(from, m + frag_row, ks, x);
-        out[p] = x[0];
-      }
-    });
+    auto take = [&](auto& out) __attribute__((always_inline)) {
+      constexpr int PLANES = kOfA ? C::A_PLANES : C::B_PLANES;
+      unroll<0, PLANES>([&](auto plane) __attribute__((always_inline)) {
+        constexpr int p = decltype(plane)::value;
+        const unsigned char* const from = tile + p * (kOfA ? C::A_PLANE : C::B_PLANE);
+        if constexpr (PLANES == 1) {
+          if constexpr (COL) read_col(from, m, ks, width, out);
+          else read_row(from, m + frag_row, ks, out);
+        } else {
+          u32x4 x[1];
+          if constexpr (COL) read_col(from, m, ks, width, x);
+          else read_row(from, m + frag_row, ks, x);
+          out[p] = x[0];
+        }
+      });
+    };
+    if constexpr (kOfA) take(f.a[q]);
+    else take(f.b[q - C::TM]);
   };
   constexpr int FRAGS = C::TM + C::TN;
   auto read = [&](int c, int ks, Frags& f) __attribute__((always_inline)) {
@@ -379,7 +384,9 @@ __device__ __forceinline__ void tile_sums(const Operand& A, const Operand& B, in
   // cubed by 256 x 256: 1,005 us, the DMAs spread 979; with A a stage ahead 900, the
   // reads spread too 878. By 64 x 64, one MFMA a step, it loses: 1,024 x 1,024 x 2,048
   // 11.0 us, spread 15.0).
-  constexpr int PRODUCTS = PARTS == 3 ? kSplitProducts : (PARTS == 2 ? 3 : 1);
+  // The last of split_device.h's products: all of them, (1,0) (0,1) (0,0), the last two or
+  // (0,0).
+  constexpr int PRODUCTS = C::MODE == kF32 ? kSplitProducts : C::A_PARTS + C::B_PARTS - 1;
   constexpr int ALL = PRODUCTS * C::TM * C::TN;
   constexpr bool kSpread = ESZ == 2 && ALL >= 4;
   auto work = [&](const Frags& cur, Frags& nxt, int c, int ks, int turn, auto from, auto to)
