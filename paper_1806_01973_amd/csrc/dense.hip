@@ -571,12 +571,12 @@ __global__ __launch_bounds__(C::THREADS, C::WPE) void dense_dw_kernel(DenseGradL
 }
 
 // dx and dW in one launch, dW's blocks first: for few rows a launch costs as much as
-// either (about 5 us). A whole backward pass, together against apart: 1,000 rows of
-// 256 -> 256 20.0 and 22.2 us (bf16), 20.1 and 27.8 (fp32); 4,596 of 512 -> 512 31.9
-// and 35.5, 61.5 and 67.9; up to 1,280 blocks, five a CU (4,596 of 512 -> 256, 1,056
-// blocks, 25.5 and 28.0, fp32 42.8 and 48.8). With many blocks the two only take cache from each other
-// (60,000 x 1,024 -> 512 in 64 equal groups 220 us, apart 108 + 80).
-constexpr int64_t kGradsTogether = 1280;
+// either (about 5 us), for many dx's first blocks run beside dW's last. A whole backward
+// pass, together and apart, us: 1,000 rows of 256 -> 256 19.4, 22.1 (bf16, no activation),
+// 19.3, 22.0 (SiLU), 21.3, 31.1 (fp32); 4,596 of 512 -> 512 25.8, 28.7; 37.1, 40.5; 71.2,
+// 79.2; 30,000 of 512 -> 512 77.9, 80.9; 112.8, 121.5; 284, 293; 300,000 of 256 -> 512
+// fp32 1,502, 1,550. It loses nowhere by more than 2% (100,000 of 1,024 -> 512 fp32 in 32
+// uneven groups 1,675, 1,645).
 template <class CX, class CW>
 __global__ __launch_bounds__(CX::THREADS, CX::WPE) void dense_grads_kernel(DenseLaunch x,
                                                                            DenseGradLaunch w,
@@ -734,20 +734,28 @@ inline int64_t tiles_of(int64_t m, int64_t n, int b) { return ((m + b - 1) / b) 
 //   bf16 128, 256: 128 tiles of 256: 16.4, 21.5; 256 tiles: 29.1, 25.1 (512 -> 512),
 //     44.6, 38.5 (1,024 -> 2,048). Up to 128 columns half of a 256-wide tile is empty:
 //     26.9, 39.0 (65,536 rows of 1,024 -> 128).
-//   bf16 groups, 1,024 -> 512: equal groups of 3,750 rows 83, 72; of 937 rows 85, 77,
-//     but uneven ones of 937 rows on average, with pre-activations, 133, 140.
-//   fp32 64, 128:  128 tiles of 128: 23.5, 31.9 (512 -> 512); 256 tiles: 39.5, 36.7.
+//   bf16 groups, forward and dx of 60,000 rows by 128, 256: 48 uneven groups (1,250 rows
+//     on average) 88, 75 (1,024 -> 512), 113, 94 (512 -> 1,024), with residual and
+//     pre-activations 124, 102 and 177, 158; 64 (937 rows) 88, 99 and 116, 111; 126, 135
+//     and 184, 179; dx 110, 103 and 86, 94, through SiLU 213, 206 and 255, 254.
+//   dx, bf16, 64, 128: 576 tiles of 64: 10.3, 11.1, through SiLU 20.8, 23.0 (dz with it);
+//     1,024 tiles: 11.1, 11.7 and 30.2, 28.7. 128, 256: 128 tiles of 256: 16.5, 21.0 and
+//     40.1, 47.3; 256 tiles: 31.1, 24.4 and 67.2, 61.4 (all 512 -> 512).
+//   fp32 64, 128:  188 tiles of 128: 22.1, 23.7 (256 -> 256); 256 tiles: 27.1, 25.4, 46.0,
+//     40.6 (512 -> 512); dx with dz, 144 tiles: 44.7, 49.7, 256 tiles: 57.0, 55.0.
 inline Shape rows_shape(const DenseLaunch& a, bool bf16) {
   const int64_t m = a.M, n = a.N;
   if (!bf16) return tiles_of(m, n, 128) < 256 ? kSmall : kMid;
   if (tiles_of(m, n, 64) <= 768) return kSmall;
-  if (n <= 128 || (a.offsets && m < 2048 * (int64_t)a.G)) return kMid;
+  if (n <= 128 || (a.offsets && m < 1024 * (int64_t)a.G)) return kMid;
   return tiles_of(m, n, 256) < 256 ? kMid : kBig;
 }
 
 // Tiles of 64 in bf16 have four stages of 16 KB, which two blocks a CU hold; where
 // there are more blocks than that, two stages, so that they run together: 576 tiles of
-// depth 512 8.5 us with two, 11.4 with four; 256 tiles of depth 2,048 18.5 and 11.4.
+// depth 512 8.5 us with two, 11.4 with four; 256 tiles of depth 2,048 18.5 and 11.4. With A
+// in two parts three stages of 24 KB or two: 576 tiles of depth 256 (dx and dW in one
+// launch, dz) 28.5 with two, 30.2 with three; 128 of depth 2,048 28.2 and 23.0.
 inline bool many(int64_t blocks) { return blocks > 512; }
 
 inline bool vectors(const void* p, int64_t ld, int64_t width, bool bf16) {
@@ -784,7 +792,7 @@ hipError_t dw_cfg(const DenseGradLaunch& a, hipStream_t s) {
 template <class CX, class CW>
 bool grads_cfg(const DenseLaunch& x, const DenseGradLaunch& w, hipStream_t s, hipError_t* e) {
   const int64_t bw = dw_blocks<CW>(w), bx = rows_blocks<CX>(x);
-  if (bw + bx > kGradsTogether) return false;
+  if (bw + bx > 0x7FFFFFFFll) return false;
   ProfileScope prof(kKDenseGrad, s);
   hipLaunchKernelGGL((dense_grads_kernel<CX, CW>), dim3((unsigned)(bw + bx)), dim3(CX::THREADS), 0, s,
                      x, w, (int)bw);
@@ -820,9 +828,11 @@ hipError_t rows_mode(const DenseLaunch& a, hipStream_t s) {
 // what the tile gains. Times of dz, dW and the sums' join in us, by 128 and by 256:
 // 300,000 rows of 1,024 -> 2,048 1,962, 1,768; 60,000 of 1,024 -> 512 126, 122, in 64
 // groups 150, 124, in uneven ones 150, 145; 4,096 of 2,048 -> 2,048 (1,024 rows a
-// block) 66, 72; 200,000 of 512 -> 256 in 32 groups (2 tiles) 160, 161. 128 x 128
-// where pieces of 512 rows fill the chip; by 64 and by 128: 60,000 of 1,024 -> 512
-// in fp32 561, 434; 20,000 of 256 -> 256 25, 28 and 44, 48.
+// block) 66, 72; 200,000 of 512 -> 256 in 32 groups (2 tiles) 160, 161. Through SiLU
+// 300,000 of 1,024 -> 512 807, 753; 60,000 181, 176, in 64 groups 205, 175, in uneven ones
+// 212, 190; 4,096 of 2,048 -> 2,048 95, 96; 100,000 of 256 -> 512 (2 tiles) 157, 163. 128 x
+// 128 where pieces of 512 rows fill the chip; by 64 and by 128: 60,000 of 1,024 -> 512
+// in fp32 712, 506; 20,000 of 256 -> 256 19, 23, through SiLU 30, 33, fp32 52, 54.
 inline Shape dw_shape(int64_t n, int N, int K, int G, bool bf16) {
   const int64_t tiles = tiles_of(N, K, 256);
   if (bf16 && tiles >= 8 && n >= 512 * (int64_t)G && n * tiles >= 1536 * 256 && N > 128 && K > 128)
@@ -844,7 +854,7 @@ hipError_t dw_mode(const DenseGradLaunch& a, hipStream_t s) {
   return shape == kSmall ? dw_cfg<typename T::Small>(a, s) : dw_cfg<typename T::Mid>(a, s);
 }
 
-// Both in one launch where both take ring tiles of four waves and are few; false: apart.
+// Both in one launch where both take ring tiles of four waves; false: apart.
 template <int MODE>
 bool grads_mode(const DenseLaunch& x, const DenseGradLaunch& w, hipStream_t s, hipError_t* e) {
   using X = Tiles<MODE, false, true>;
@@ -864,8 +874,8 @@ bool grads_mode(const DenseLaunch& x, const DenseGradLaunch& w, hipStream_t s, h
 
 // Few rows: the weight goes through registers once, without LDS tiles. Times in us, by
 // this kernel and by tiles of 64. fp32, whose tiles split each weight first: up to 128
-// rows (512 -> 512 1 row 6.1, 13.2, 128 rows 12.2, 14.4, 256 rows 22.9, 14.5), or 16
-// a group on average (64 groups, 1,024 rows 20.1, 22.3, 2,048 rows 32.4, 23.2). bf16:
+// rows (512 -> 512 16 rows 6.3, 15.8, 128 rows 12.3, 16.2, 192 rows 17.6, 16.3), or 16
+// a group on average (64 groups, 1,024 rows 20.4, 25.9, 2,048 rows 32.7, 26.1). bf16:
 // up to 32 rows (2,048 -> 4,096 8 rows 6.1, 9.7, 64 rows 11.6, 9.9), or 16 a group
 // in one round of blocks (8 groups, 1,024 -> 1,024, 128 rows 6.5, 7.1; 16 groups,
 // 2,048 -> 1,024, two rounds, 16.4, 12.5). A group that has most of the rows takes

@@ -307,12 +307,11 @@ __device__ __forceinline__ void multiply_parts(const Parts8& b, const Parts8& l,
 // ---- medium matrices: A's square and its product with Y in one launch -------------------
 // Y (a I + b A + c A A) = a Y + b T + c T A with T = Y A: a block holds A and 32 rows of Y in
 // LDS, forms T in Y's place (rounded as Y is) and Y's successor from it. Against the two
-// launches (B, then Y B) it multiplies more, 4 m^2 n against m^3 + 2 m^2 n, but up to 256
-// columns (128 in two parts), where A fits beside Y, launches and loads are what costs:
-// 6.5 us for 8 matrices of 256 x 512 where the two take 9.3. Whole calls in us, with it
-// and without: bf16 128 x 512 56, 71; 4 of 100 x 1,000 66, 82; 8 of 256 x 512 69, 80; 8 of
-// 256 x 2,048 127, 129; fp32 128 x 512 76, 95; 8 of 128 x 2,048 147, 162. The width is a
-// compile-time constant: at run time its divisions alone took 3 us.
+// launches (B, then Y B) it multiplies more, 4 m^2 n against m^3 + 2 m^2 n, but up to 128
+// columns, where A fits beside Y, launches and loads are what costs. Whole calls in us,
+// with it and without: 64 x 384 63, 79; 128 x 512 79, 95; 4 of 100 x 1,000 102, 119; 32 of
+// 128 x 512 102, 113; 8 of 128 x 2,048 153, 163. The width is a compile-time constant: at
+// run time its divisions alone took 3 us.
 constexpr int kBandWaves = 8, kBandRows = 32;
 
 template <int mp>
@@ -418,9 +417,8 @@ __global__ __launch_bounds__(64 * kBandWaves) void newton_band_kernel(NewtonLaun
 // ---- small matrices: everything in one block ------------------------------------------
 // A block of eight waves takes a matrix from G to the result, X and one m x m matrix in
 // its LDS: what bounds a small matrix else is that there are 13 launches, at 3 to 5 us
-// each whatever they compute. In two parts always. Up to 64 x 320, us, one block and
-// launches: 64 x 64 25, 49; 512 of them 53, 84; 300 x 40 49, 60; 64 x 320 58, 61;
-// 64 x 384 67, 63; fp32 128 x 128 72, 63.
+// each whatever they compute. Up to 64 x 320, us, one block and launches: 64 x 64 26, 50;
+// 512 of them 55, 89; 300 x 40 51, 61; 64 x 320 59, 62; 64 x 384 67, 63; 128 x 128 72, 63.
 // X [mp][np] and A [mp][mp] lie in LDS in fp16 parts; X's columns, for B X, come through
 // transposing reads. A wave's blocks of 32 x 32 stay in its accumulators until all waves
 // have read what they replace.
@@ -619,18 +617,19 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
 }
 
 // ---- tile shapes --------------------------------------------------------------------
-// Measured at depth 2,048, us (fp16): 64 x 64 tiles with four stages, two blocks per
-// CU, 10.8 at 256 tiles and 23.8 at 529; with two stages, which more of them share a
-// CU, 18.4, 20.8 and 27.8 at 1,024; 128 x 128 with four stages 23.9 at 256 tiles (as
-// 1,024 of 64 x 64), with two 28.2, but 75 against 103 at 1,876 tiles of depth 1,024.
-// Two parts: 64 x 64 with four stages 19.3 at 256 tiles, with two 24.3 and 59.6 at
-// 1,024, 128 x 128 57.0.
+// 64 x 64 with four stages (128 KB, a block a CU) while the tiles are no more than CUs,
+// with two stages, which more of them share, up to 600 tiles, else 128 x 128. Whole calls
+// in us. Four stages, two: 1,024 x 1,024 (136 and 256 tiles) 200, 234; 1,024 x 2,048's 512
+// tiles 296, 272. 64, 128 for the symmetric products: 435 tiles (1,800 x 1,800) 569, 690;
+// 544 (4 of 1,024 x 1,024) 476, 479; 576 (16 of 512 x 512) 311, 330; 528 deep ones (2,048 x
+// 2,048) 827, 785. For Y B: 484 tiles (1,408 x 1,408) 320, 356; 625 (1,600 x 1,600) 486,
+// 459; 768 (3 of 1,024 x 1,024) 364, 352; 1,024 (2,048 x 2,048) 875, 827.
 inline int64_t tiles_of(const NewtonWork& w, int64_t batch, bool symmetric, int side) {
   const int64_t tm = (w.mp + side - 1) / side, tn = (w.np + side - 1) / side;
   return (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batch;
 }
 inline bool small_tiles(const NewtonWork& w, int64_t batch, bool symmetric) {
-  return tiles_of(w, batch, symmetric, 64) <= 1024;
+  return tiles_of(w, batch, symmetric, 64) <= 600;
 }
 
 template <class C, int KIND, bool BF16>
