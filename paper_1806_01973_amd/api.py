@@ -596,7 +596,8 @@ def dense_forward(x: torch.Tensor, W: torch.Tensor, b: Optional[torch.Tensor] = 
     W[g] of W [groups, d_out, d_in] and b[g]; rows past the last group become zero. x, W and the
     residual share one dtype, float32 or bfloat16; matrices may have any row stride. activation:
     "none", "relu", "gelu" (tanh form) or "silu". Returns y, or (y, u) with want_preact, u the
-    value before the activation, which dense_backward needs."""
+    value before the activation, which dense_backward needs. There is no autograd function: the
+    results do not require gradients, whatever the inputs do; the caller runs dense_backward."""
     d = _dense(x.dtype, W, b, activation, offsets)
     n = int(x.shape[0])
     ldx = _rows(x, "x", n, d.d_in, x.dtype)
@@ -624,7 +625,7 @@ def dense_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor,
     """Gradients (dx, dW, db) of dense_forward for dy, the loss's gradient by y (it is the
     residual's gradient as well); u is the pre-activation that the forward pass kept (not needed
     without an activation). Entries that are not needed are None. db is fp32, dx and dW have x's
-    dtype."""
+    dtype; none of them requires gradients."""
     d = _dense(x.dtype, W, None, activation, offsets)
     n = int(x.shape[0])
     ldx = _rows(x, "x", n, d.d_in, x.dtype)
@@ -689,7 +690,8 @@ def orthogonalize(g: torch.Tensor, steps: int = 5, coefficients=NEWTON_SCHULZ, e
                   stream=None) -> torch.Tensor:
     """Newton-Schulz orthogonalisation of g [rows, cols] or of each g[i] of [batch, rows, cols]:
     X = g / (|g|_F + eps), then `steps` times X = a X + (b A + c A A) X with A = X X^T (in the
-    orientation with fewer rows than columns)."""
+    orientation with fewer rows than columns). Coefficients that can take X, A, b A + c A A or
+    A X past 15.5 are refused. The result does not require gradients."""
     p = _newton_schulz(g, "g", steps, coefficients, eps)
     if out is None:
         out = _empty(g.shape, g.dtype, g.device, stream)

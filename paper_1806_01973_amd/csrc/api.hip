@@ -1758,7 +1758,8 @@ DenseWs dense_ws(const pinsage_dense_t* d, int64_t n) {
     w.dz_plane = (int64_t)w.dz;
     w.dz *= 2;
   }
-  w.db = align_up((size_t)dense_bias_pieces(n, d->num_groups, dense_bias_rows(n, d->d_out, d->dtype == PINSAGE_BF16)) * d->d_out * 4);
+  const int bias_rows = dense_bias_rows(n, d->d_out, d->dtype == PINSAGE_BF16);
+  w.db = align_up((size_t)dense_bias_pieces(n, d->num_groups, bias_rows) * d->d_out * 4);
   w.dw = align_up((size_t)dense_dw_parts(n, w.piece, d->num_groups) * d->d_out * d->d_in * 4);
   return w;
 }

@@ -204,8 +204,9 @@ struct Groups {
 // edges, middling ones by the edges (loads until the first chunk is there, the epilogue's
 // reads and writes), small ones by the launch. bf16: 300,000 rows of 1,024 -> 2,048
 // 1.28-1.33 ms (945-985 TFLOP/s; 48% of the cycles have MFMAs, at 1.88 GHz of 2.4); 60,000 of
-// 1,024 -> 512 in 64 groups with residual and pre-activations 125-130 us (2.9 TB/s). fp32:
-// 4,596 of 512 -> 512 32 us; dx of 100,003 rows of 512 -> 256 183 us (143 TFLOP/s).
+// 1,024 -> 512 in 64 groups with residual and pre-activations 125-130 us (2.9 TB/s); its
+// dx with dz in two parts 178 us (33% of the cycles have MFMAs). fp32: 4,596 of 512 -> 512
+// 39 us; dx and dW of 100,003 rows of 256 -> 512 in one launch 400 us (131 TFLOP/s, 53%).
 template <class C>
 __device__ __forceinline__ void rows_block(const DenseLaunch& a, int block, int blocks,
                                            unsigned char* smem) {
@@ -435,7 +436,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void dense_few_kernel(DenseLaunch a
 // A block takes a piece of a.bias_rows rows of one group; `lanes` threads (the
 // smallest power of two that covers the columns, 64 at most) lie side by side along a
 // row, 16 bytes each, over (256 / lanes) rows at once, four such in flight. Bound by
-// memory: it reads dy and u and writes dz once (100,003 x 512 fp32 115 us, 5.3 TB/s).
+// memory: it reads dy and u and writes dz once (100,003 x 512 fp32 118 us, 5.2 TB/s;
+// 60,000 x 512 bf16, dz in two parts, 54 us, 4.6 TB/s).
 template <bool BF16>
 __global__ __launch_bounds__(256) void dense_dz_kernel(DenseGradLaunch a, int lanes) {
   constexpr int ESZ = BF16 ? 2 : 4, V = 16 / ESZ, DEEP = 4;
@@ -514,8 +516,8 @@ __global__ __launch_bounds__(256) void dense_dz_kernel(DenseGradLaunch a, int la
 // dW[g][n][k] = sum over the group's rows of dz[r][n] x[r][k]. Where the tiles of
 // dW alone leave CUs idle, a group's rows are cut into pieces of a.piece rows; a
 // group of several leaves fp32 partial sums in the workspace, which
-// dense_join_kernel adds in order. 100,003 rows of 256 -> 512 fp32 158 us (166 TFLOP/s),
-// 60,000 of 1,024 -> 512 bf16 in 64 uneven groups 94 us (670 TFLOP/s).
+// dense_join_kernel adds in order. 60,000 rows of 1,024 -> 512 bf16 in 64 uneven groups
+// 94 us (670 TFLOP/s), with dz in two parts 137 us (42% of the cycles have MFMAs).
 template <class C>
 __device__ __forceinline__ void dw_block(const DenseGradLaunch& a, int block, int blocks,
                                          unsigned char* smem) {
@@ -591,7 +593,7 @@ __global__ __launch_bounds__(CX::THREADS, CX::WPE) void dense_grads_kernel(Dense
 // The partial sums, added in order: of dW (blocks below dw_blocks) and of db. An item
 // is 256 elements of a group that has partial sums; `shares` (1, 4 or 16) of a
 // block's 16 waves add its pieces, in order within each and then over the shares.
-// Bound by the latency of few reads each: 33 MB of 100,003 rows of 256 -> 512 fp32 22 us.
+// Bound by the latency of few reads each: 33 MB of 100,003 rows of 256 -> 512 fp32 23 us.
 constexpr int kJoinWaves = 16;
 template <bool BF16>
 __global__ __launch_bounds__(64 * kJoinWaves) void dense_join_kernel(DenseGradLaunch a,
@@ -825,14 +827,13 @@ hipError_t rows_mode(const DenseLaunch& a, hipStream_t s) {
 
 // Tiles of dW. 256 x 256 (bf16) where there are 8 of them or more and one round of
 // blocks takes 1,536 rows each or more: with fewer of either, the partial sums cost
-// what the tile gains. Times of dz, dW and the sums' join in us, by 128 and by 256:
-// 300,000 rows of 1,024 -> 2,048 1,962, 1,768; 60,000 of 1,024 -> 512 126, 122, in 64
-// groups 150, 124, in uneven ones 150, 145; 4,096 of 2,048 -> 2,048 (1,024 rows a
-// block) 66, 72; 200,000 of 512 -> 256 in 32 groups (2 tiles) 160, 161. Through SiLU
-// 300,000 of 1,024 -> 512 807, 753; 60,000 181, 176, in 64 groups 205, 175, in uneven ones
-// 212, 190; 4,096 of 2,048 -> 2,048 95, 96; 100,000 of 256 -> 512 (2 tiles) 157, 163. 128 x
-// 128 where pieces of 512 rows fill the chip; by 64 and by 128: 60,000 of 1,024 -> 512
-// in fp32 712, 506; 20,000 of 256 -> 256 19, 23, through SiLU 30, 33, fp32 52, 54.
+// what the tile gains. Times of dW and the sums' join in us, by 128 and by 256, and the
+// same with dz through SiLU: 300,000 rows of 1,024 -> 512 364, 289 and 807, 753; 60,000
+// 81, 82 and 181, 176, in 64 groups 97, 81 and 205, 175, in uneven ones 107, 99 and 212,
+// 190; 4,096 of 2,048 -> 2,048 (1,024 rows a block) 54, 57 and 95, 96; 100,000 of
+// 256 -> 512 (2 tiles) 47, 53 and 157, 163. 128 x 128 where pieces of 512 rows fill the
+// chip; by 64 and by 128: 60,000 of 1,024 -> 512 135, 81 and, fp32 with dz, 712, 506;
+// 20,000 of 256 -> 256 19, 23, through SiLU 30, 33, fp32 52, 54.
 inline Shape dw_shape(int64_t n, int N, int K, int G, bool bf16) {
   const int64_t tiles = tiles_of(N, K, 256);
   if (bf16 && tiles >= 8 && n >= 512 * (int64_t)G && n * tiles >= 1536 * 256 && N > 128 && K > 128)
@@ -906,8 +907,9 @@ hipError_t launch_dense_rows(const DenseLaunch& a, hipStream_t s) {
 
 // Rows per piece of dW's sums: pieces that give every CU one round of blocks (one
 // block of 256 x 256, two of the others), of 256 rows at least. More and smaller ones
-// even out uneven groups but cost partial sums: 60,000 rows of 1,024 -> 512 in 64
-// uneven groups 145 us, with pieces half as long 194.
+// even out uneven groups but cost partial sums: whole, half and a quarter as long, us:
+// 200,000 rows of 512 -> 512 bf16 in 32 uneven groups through SiLU 384, 400, 426; 60,000
+// of 512 -> 256 fp32 in 64 183, 186, 217.
 int64_t dense_dw_piece(int64_t n, int N, int K, int G, bool bf16) {
   const Shape shape = dw_shape(n, N, K, G, bf16);
   const int64_t tiles = tiles_of(N, K, side(shape));

@@ -74,7 +74,7 @@ __device__ __forceinline__ float value(const Parts8& x, int e) {
 // ---- the norm, with the momentum's update ---------------------------------------
 // What is orthogonalised, elements at .. at + 3 of the batch's storage: the input,
 // or the step's combination of it with the already updated momentum. The norm of
-// 2,048 x 2,048 bf16 with its momentum takes 9 us (42 MB, 4.7 TB/s), Y0 9 us.
+// 2,048 x 2,048 bf16 with its momentum takes 9 us (42 MB, 4.7 TB/s), Y0 11 us.
 template <bool BF16>
 __device__ __forceinline__ void update4(const NewtonLaunch& a, int64_t at, int cols, float (&u)[4]) {
   read_row<BF16>(a.in, at, cols, u);
@@ -162,10 +162,12 @@ __global__ __launch_bounds__(256) void newton_start_kernel(NewtonLaunch a, Newto
 enum NewtonProduct { kGram = 0, kSquare = 1, kApply = 2, kLast = 3 };
 
 // P[i][j] = sum_k L(i, k) R(j, k): Y^T Y, A A, or Y B (A and B are symmetric). About 8 us
-// of each are its launch, first loads and epilogue; the rest is bound by what the tiles
-// load (64 x 64: 16 to 20 TB/s out of the L2s; order of tiles and row pitch make no
-// difference). 2,048 x 2,048 in one part 24, 23 and 26 us (the last 660 TFLOP/s), 2,048 x
-// 1,024 in two parts 20, 12 and 19 us.
+// of each are its launch, first loads and epilogue; the rest waits for the tiles' loads,
+// the MFMAs have 20% of the cycles by 64 x 64 and 42% by 128 x 128. By the counters 64 x 64
+// tiles take 10 to 12 TB/s out of the L2s, well below what those serve, so the latency of
+// two stages bounds them; order of tiles and row pitch make no difference. 2,048 x 2,048
+// 54, 54 (528 tiles of 64, 550 MB each) and 57 us (256 of 128, 545 MB), 2,048 x 1,024 20,
+// 13 (136 tiles on 256 CUs, 134 and 69 MB) and 19 us (512 tiles, 225 MB).
 template <class C, int KIND, bool BF16>
 __global__ __launch_bounds__(C::THREADS, C::WPE) void newton_kernel(NewtonLaunch a, NewtonWork w,
                                                                     int from, int tiles) {
@@ -295,13 +297,19 @@ __device__ __forceinline__ Parts8 lds_fragment(const unsigned char* M, int pitch
 }
 // All products of the parts, lo lo too: the diagonal of A sums squares, so what is left
 // out has one sign, which shows with few singular values (fp32, 16 x 100, 4 draws: mean
-// error 1.3e-6, with lo lo 1.0e-6).
-__device__ __forceinline__ void multiply_parts(const Parts8& b, const Parts8& l,
-                                               f32x16& acc) {
-  acc = product_mfma<kF16x2>(b.p[1], l.p[1], acc);
-  acc = product_mfma<kF16x2>(b.p[1], l.p[0], acc);
-  acc = product_mfma<kF16x2>(b.p[0], l.p[1], acc);
-  acc = product_mfma<kF16x2>(b.p[0], l.p[0], acc);
+// error 1.3e-6, with lo lo 1.0e-6). hi hi has sums of its own.
+struct PartSums {
+  f32x16 large, small;
+  __device__ __forceinline__ void clear() {
+    clear_block(large);
+    clear_block(small);
+  }
+};
+__device__ __forceinline__ void multiply_parts(const Parts8& b, const Parts8& l, PartSums& acc) {
+  acc.small = product_mfma<kF16x2>(b.p[1], l.p[1], acc.small);
+  acc.small = product_mfma<kF16x2>(b.p[1], l.p[0], acc.small);
+  acc.small = product_mfma<kF16x2>(b.p[0], l.p[1], acc.small);
+  acc.large = product_mfma<kF16x2>(b.p[0], l.p[0], acc.large);
 }
 
 // ---- medium matrices: A's square and its product with Y in one launch -------------------
@@ -359,11 +367,13 @@ __global__ __launch_bounds__(64 * kBandWaves) void newton_band_kernel(NewtonLaun
   const float back = 1.0f / kScale;  // products carry the scale twice
   f32x16 acc;
   auto product = [&]() __attribute__((always_inline)) {
-    clear_block(acc);
+    PartSums sums;
+    sums.clear();
 #pragma unroll
     for (int ks = 0; ks < mp / 16; ++ks)
       multiply_parts(lds_fragment(lds_a, pitch, plane_a, 32 * wave, ks),
-                             lds_fragment(lds_y, pitch, plane_y, 0, ks), acc);
+                     lds_fragment(lds_y, pitch, plane_y, 0, ks), sums);
+    acc = sums.large + sums.small;
   };
   // The lane's columns 8 g + 4 (lane / 32) of the wave's, row i of the band.
   auto place = [&](int g) __attribute__((always_inline)) {
@@ -517,7 +527,8 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
   };
   // Block (bi, bj) of M becomes p M + q sum.
   auto update = [&](unsigned char* M, int pitch, int plane, int bi, int bj, float p, float q,
-                    const f32x16& sum) __attribute__((always_inline)) {
+                    const PartSums& parts) __attribute__((always_inline)) {
+    const f32x16 sum = parts.large + parts.small;
     const int i = 32 * bi + frag_row;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
@@ -542,13 +553,13 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
     }
   };
   const float back = 1.0f / kScale;  // products carry the scale twice
-  f32x16 acc[kSmallBlocks];
+  PartSums acc[kSmallBlocks];
 
   for (int step = 0; step < a.steps; ++step) {
     // A = X X^T, a wave's blocks in turn.
     for (int b = wave; b < mb * mb; b += kSmallWaves) {
       const int bi = b / mb, bj = b % mb;
-      clear_block(acc[0]);
+      acc[0].clear();
       for (int ks = 0; ks < np / 16; ++ks)
         multiply_parts(lds_fragment(X, np * 2, px, 32 * bj, ks),
                        lds_fragment(X, np * 2, px, 32 * bi, ks), acc[0]);
@@ -557,7 +568,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
     __syncthreads();
     // A becomes b A + c A A (A is symmetric: both operands are its rows).
 #pragma unroll
-    for (int t = 0; t < kSmallBlocks; ++t) clear_block(acc[t]);
+    for (int t = 0; t < kSmallBlocks; ++t) acc[t].clear();
     for (int ks = 0; ks < mp / 16; ++ks)
 #pragma unroll
       for (int t = 0; t < kSmallBlocks; ++t) {
@@ -575,7 +586,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void newton_small_kernel(NewtonLa
     __syncthreads();
     // X becomes a X + A X.
 #pragma unroll
-    for (int t = 0; t < kSmallBlocks; ++t) clear_block(acc[t]);
+    for (int t = 0; t < kSmallBlocks; ++t) acc[t].clear();
     for (int ks = 0; ks < mp / 16; ++ks)
 #pragma unroll
       for (int t = 0; t < kSmallBlocks; ++t) {

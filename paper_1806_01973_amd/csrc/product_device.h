@@ -10,8 +10,8 @@
 //   kBf16A2 the same, A in two bf16 parts (planes apart by `plane` bytes: 16
 //           significand bits), two MFMAs (lo, hi)
 //   kF16x2  two fp16 parts in memory (x = hi + lo, planes apart by `plane`
-//           bytes): 22 significand bits, three MFMAs (hi lo, lo hi, hi hi); for
-//           operands the caller keeps inside fp16's range
+//           bytes): 22 significand bits, three MFMAs (hi lo, lo hi, hi hi, the last
+//           in sums of its own); for operands the caller keeps inside fp16's range
 //   kF32    fp32 in memory, split on the way to the MFMAs into three bf16 parts (24
 //           significand bits), eight MFMAs, the leading products in sums of their
 //           own: what is left out is below 2^-33 of a product (split_device.h).

@@ -25,10 +25,11 @@
 //
 // What bounds large products are the MFMAs, in 63% of the cycles of 8,192 cubed by
 // 256 x 256 (counted when it took 943 us; it takes 878), and the clock, which power holds
-// at 1.76 GHz of 2.4; the LDS serves fragments in a quarter of the cycles. With every tile's operands in L2 the same product
-// takes 11% less. Smaller tiles are bound by their loads, 64 x 64 at 16 to 20 TB/s out of
-// the L2s. Waves that share a tile's k steps, so that smaller tiles keep larger wave
-// tiles, gained 5% at most and are not here.
+// at 1.76 GHz of 2.4; the LDS serves fragments in a quarter of the cycles. With every
+// tile's operands in L2 the same product takes 11% less. Smaller tiles wait for their
+// loads, 64 x 64 at 10 to 12 TB/s out of the L2s in Newton-Schulz. Waves that share a
+// tile's k steps, so that smaller tiles keep larger wave tiles, gained 5% at most and are
+// not here.
 // Where rows end inside a tile, lanes read the last row or vector again (the
 // results of those rows are never used); past the end of k they read zeros.
 // bf16, 300,000 x 1,024 -> 2,048 by 256 x 256 1,332 us (945 TFLOP/s), the epilogue with
@@ -147,9 +148,11 @@ __device__ __forceinline__ void tile_sums(const Operand& A, const Operand& B, in
   for (int i = 0; i < C::TM; ++i)
 #pragma unroll
     for (int j = 0; j < C::TN; ++j) clear_block(acc[i][j]);
-  // kF32: the sums of the products of parts beside the leading one.
-  f32x16 small[C::MODE == kF32 ? C::TM : 1][C::TN];
-  if constexpr (C::MODE == kF32)
+  // The products of parts beside the leading one have sums of their own, so that the large
+  // ones round once a step (bf16 results need none).
+  constexpr bool kApart = C::MODE == kF32 || C::MODE == kF16x2;
+  f32x16 small[kApart ? C::TM : 1][C::TN];
+  if constexpr (kApart)
 #pragma unroll
     for (int i = 0; i < C::TM; ++i)
 #pragma unroll
@@ -403,7 +406,7 @@ __device__ __forceinline__ void tile_sums(const Operand& A, const Operand& B, in
       constexpr int e = decltype(at)::value, q = e / (C::TM * C::TN), i = e / C::TN % C::TM,
                     j = e % C::TN;
       constexpr int t = kSplitProducts - PRODUCTS + q, pb = split_b(t), pa = split_a(t);
-      f32x16& sum = C::MODE == kF32 && q < PRODUCTS - 1 ? small[C::MODE == kF32 ? i : 0][j] : acc[i][j];
+      f32x16& sum = kApart && q < PRODUCTS - 1 ? small[kApart ? i : 0][j] : acc[i][j];
       sum = product_mfma<C::MODE>(cur.b[j][pb], cur.a[i][pa], sum);
       if constexpr (kSpread) {
         constexpr int r0 = (e * FRAGS + ALL - 1) / ALL, r1 = ((e + 1) * FRAGS + ALL - 1) / ALL;
@@ -495,11 +498,12 @@ __device__ __forceinline__ void tile_sums(const Operand& A, const Operand& B, in
   }
   if constexpr (!C::REGS) ring_wait<0>();
   bool covered = true;
-  if constexpr (C::MODE == kF32) {
+  if constexpr (kApart)
 #pragma unroll
     for (int i = 0; i < C::TM; ++i)
 #pragma unroll
       for (int j = 0; j < C::TN; ++j) acc[i][j] += small[i][j];
+  if constexpr (C::MODE == kF32) {
     // Infinities, NaN and values or sums that round to an infinity show in the results.
     float probe = 0.0f;
 #pragma unroll
