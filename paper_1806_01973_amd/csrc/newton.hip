@@ -11,8 +11,8 @@
 // 480 times, and what is rounded off X, A and B in their place with them: of a bf16
 // matrix of rank 1 (16) one part's 2^-11 leaves an error of 9.5e-2 (3.8e-2), two parts
 // 1.6e-3 as the formula in fp32 does, which is bf16's own rounding of the result. fp32
-// of rank 1: 2.7e-5, the formula in fp32 1.3e-4. Sums, and a X, run in
-// fp32; |G|_F is summed in fp64, so no finite G overflows.
+// 256 x 512 of rank 1: 6.3e-5, the formula in fp32 1.4e-4. Sums, and a X, run in fp32;
+// |G|_F is summed in fp64, so no finite G overflows.
 // Y = X^T, A and B live in the workspace, padded with zeros to whole tiles, so that
 // no product has an edge: A = Y^T Y (both operands by columns), A A, and
 // Y = a Y + Y B. A and A A are symmetric: only their tiles on and above the diagonal
