@@ -559,9 +559,9 @@ int pinsage_dense_backward(const pinsage_dense_t* layer, const void* dy, int64_t
  * themselves (two fp16 parts around a fixed scale), whatever the storage type; the
  * steps enlarge small singular directions about 480 times and these roundings with
  * them (fp32, 256 x 512 of rank 1: 6.3e-5 of the result, where the formula in
- * fp32 leaves 1.4e-4). Coefficients that can take X, A, b A + c A A or A X of some matrix past
- * 15.5 within `steps` are refused (PINSAGE_EUNSUPPORTED): the parts end at 16. A
- * matrix whose norm is far below eps loses low bits (absolute 2^-36 of X).
+ * fp32 leaves 1.4e-4). Coefficients that can take X, A, b A + c A A or A X of some
+ * matrix past 15.5 within `steps` are refused (PINSAGE_EUNSUPPORTED): the parts end
+ * at 16. A matrix whose norm is far below eps loses low bits (absolute 2^-36 of X).
  * Limits: 1 <= rows, cols <= 16384, 1 <= steps <= 64, batch <= 65535. */
 typedef struct {
   int64_t batch;
